@@ -277,6 +277,146 @@ raas_status raas_set_attention_splits(raas_pool* pool, int32_t splits);
 raas_status raas_profile(raas_pool* pool, int32_t mask);
 raas_status raas_profile_read(raas_pool* pool, int32_t kernel, double* total_ms, int64_t* launches);
 
+/* ------------------------------------------------------------------------
+ * A cache that evicts by accumulated attention weight (the heavy-hitter
+ * policy that the paper compares with), token by token: a unit holds at most
+ * `capacity` tokens, prompt tokens among them, and every token carries the sum
+ * of the attention probabilities that the unit's G query heads have given it.
+ * With n tokens held, a decode step of a unit
+ *   1. stores the new token in place n while n < capacity; in a full cache it
+ *      takes the place of the token with the least weight (of equal ones the
+ *      oldest) among those older than the `recent` newest;
+ *   2. computes softmax attention of the G query heads over the held tokens,
+ *      the new one included (scale 1/sqrt(head_dim)), and over a shared
+ *      prefix besides, if one is given;
+ *   3. adds to every held token's weight its probabilities in that softmax,
+ *      summed over the G heads (fp32; the new token's start at 0).
+ * The conventions above hold: device tensors (aligned to their element type),
+ * head-major layouts, nothing awaited (but by the export and the destroys),
+ * finite inputs, calls on one handle ordered. Outputs are bitwise
+ * reproducible. Steps, prefix attention and prompt weights allocate nothing
+ * and copy nothing from the host, so they may be captured into a HIP graph,
+ * and a replay works on what the cache and the prefix hold then; graphs of one
+ * handle are ordered like its calls (they share its scratch). A handle's calls
+ * run on the device that was current at its creation. */
+typedef struct {
+    int32_t batch;      /* sequences, >= 1; batch * n_kv_heads <= 1000000 */
+    int32_t n_layers;   /* >= 1 */
+    int32_t n_q_heads;  /* multiple of n_kv_heads, group G = n_q_heads/n_kv_heads <= 16 */
+    int32_t n_kv_heads; /* 1 .. 65535 */
+    int32_t head_dim;   /* 64 or 128 */
+    int32_t capacity;   /* tokens per unit, 2 .. 1048576 */
+    int32_t recent;     /* newest tokens that are never evicted, 0 .. capacity - 1 */
+    int32_t dtype;      /* raas_dtype of q, k, v and out */
+} raas_weight_config;
+
+typedef struct raas_weight_cache raas_weight_cache; /* opaque */
+
+/* One prompt that a batch shares, stored once per layer and KV head. */
+typedef struct {
+    int32_t n_layers, n_q_heads, n_kv_heads, head_dim; /* as above */
+    int32_t max_tokens; /* tokens that a layer may store, 1 .. 1048576 */
+    int32_t max_rows;   /* sequences per call, >= 1; max_rows * n_q_heads <= 16777216 */
+    int32_t dtype;      /* raas_dtype */
+} raas_prefix_config;
+
+typedef struct raas_prefix raas_prefix; /* opaque */
+
+/* Validates cfg, allocates the cache in device memory and clears it on
+ * `stream`. The caller releases it with raas_destroy_weight_cache. Errors:
+ * RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_HIP. */
+raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream, raas_weight_cache** out);
+
+/* Synchronises the cache's last stream and frees it. NULL is ignored. */
+void raas_destroy_weight_cache(raas_weight_cache* cache);
+
+/* Device bytes the cache holds; fixed from creation on. */
+size_t raas_weight_cache_bytes(const raas_weight_cache* cache);
+
+/* (Re)starts sequences of one layer with their prompts. Sequence b has the
+ * first lens[b] tokens (HOST int32 [batch], each in [0, max_len]; NULL: all
+ * have max_len) of k, v [batch][n_kv_heads][max_len][head_dim] (NULL allowed
+ * when no selected sequence has a token), and the weights of weights
+ * [batch][n_kv_heads][max_len] (fp32; NULL: 0; raas_prompt_weights computes
+ * them). A prompt longer than the capacity keeps its `recent` newest tokens and
+ * the heaviest others (of equal ones the newer). seq_mask: optional HOST int32
+ * [batch]; only sequences with a nonzero entry are started, the others keep
+ * their state. The first prefill of a layer must cover every sequence (else
+ * RAAS_E_STATE). Errors: RAAS_E_INVALID, RAAS_E_STATE, RAAS_E_HIP. */
+raas_status raas_weight_prefill(raas_weight_cache* cache, int32_t layer, const void* k, const void* v,
+                                const float* weights, const int32_t* lens, const int32_t* seq_mask, int32_t max_len,
+                                void* stream);
+
+/* One decode step of one layer (1-3 above). q [batch][n_q_heads][head_dim];
+ * k_new, v_new [batch][n_kv_heads][head_dim]; out
+ * [batch][n_q_heads][head_dim]. Optional outputs (NULL = not written), per unit
+ * and place, after the step:
+ *   positions_out [u][capacity]: absolute position of the token, -1 if free;
+ *   weights_out   [u][capacity]: its weight (fp32), 0 if free;
+ *   evicted_out   [u]          : position of the token that this step evicted, or -1.
+ * active: optional DEVICE int32 [batch]; sequences with a zero entry take no
+ * step: their state and rows of the outputs stay as they are. prefix: NULL, or
+ * a shared prefix of the same heads, head_dim, dtype and device, whose layer of
+ * the same index has been stored and whose max_rows covers the batch (its
+ * scratch is used: the call counts as one of the prefix's too). Errors:
+ * RAAS_E_INVALID, RAAS_E_STATE (layer not prefilled, prefix not stored),
+ * RAAS_E_HIP. */
+raas_status raas_weight_step(raas_weight_cache* cache, int32_t layer, const void* q, const void* k_new,
+                             const void* v_new, void* out, int32_t* positions_out, float* weights_out,
+                             int32_t* evicted_out, const int32_t* active, raas_prefix* prefix, void* stream);
+
+/* Copies one layer's positions [u][capacity], weights [u][capacity] and clocks
+ * [u] (the position of the next token) to host memory (synchronises `stream`).
+ * Errors: RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_HIP. */
+raas_status raas_weight_export_state(raas_weight_cache* cache, int32_t layer, int32_t* positions, float* weights,
+                                     int32_t* clocks, void* stream);
+
+/* As raas_create_weight_cache, for a shared prefix. */
+raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas_prefix** out);
+
+/* Synchronises the prefix's last stream and frees it. NULL is ignored. */
+void raas_destroy_prefix(raas_prefix* prefix);
+
+/* Device bytes the prefix holds; fixed from creation on. */
+size_t raas_prefix_bytes(const raas_prefix* prefix);
+
+/* Stores `tokens` (0 .. max_tokens) tokens, k, v [n_kv_heads][tokens]
+ * [head_dim], as one layer's prefix, in the place of what it held. Errors:
+ * RAAS_E_INVALID, RAAS_E_HIP. */
+raas_status raas_prefix_store(raas_prefix* prefix, int32_t layer, const void* k, const void* v, int32_t tokens,
+                              void* stream);
+
+/* Softmax attention of q [rows][n_q_heads][head_dim] (rows: 0 .. max_rows) over
+ * the layer's prefix: out [rows][n_q_heads][head_dim] in the prefix's dtype,
+ * and, unless NULL, lse [rows][n_q_heads] (fp32): the natural logarithm of the
+ * sum of the exponentials of the scaled logits. Over an empty prefix out is 0
+ * and lse -inf. Errors: RAAS_E_INVALID, RAAS_E_STATE (layer not stored),
+ * RAAS_E_HIP. */
+raas_status raas_prefix_attention(raas_prefix* prefix, int32_t layer, const void* q, int32_t rows, void* out,
+                                  float* lse, void* stream);
+
+/* The weights that a prompt's own queries give its tokens: for sequence b of
+ * lens[b] tokens (HOST int32 [batch], each in [0, max_len]; NULL: max_len) and
+ * its last n = min(window, lens[b]) queries, weights[b][h][j] is the sum over
+ * these queries and the heads of group h of the causal softmax's probability
+ * of token j. q [batch][window][n_q_heads][head_dim] holds the queries of
+ * positions lens[b] - n .. lens[b] - 1 in its rows 0 .. n - 1 (with window =
+ * max_len: those of every token, in order); k
+ * [batch][n_kv_heads][max_len][head_dim]; weights [batch][n_kv_heads][max_len]
+ * (fp32; entries from lens[b] on are not written). prefix_lse: NULL, or fp32
+ * [batch][window][n_q_heads], the log-sum-exp of the same queries over a shared
+ * prefix in front of the prompt (raas_prefix_attention), which the softmax
+ * then counts. window lies in [1, max(1, max_len)]. workspace: device memory of
+ * at least raas_prompt_weights_workspace bytes (0 for invalid sizes), which
+ * calls that overlap must not share. The tensors lie on the current device.
+ * Errors: RAAS_E_INVALID, RAAS_E_HIP. */
+size_t raas_prompt_weights_workspace(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len,
+                                     int32_t window);
+raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                const void* q, const void* k, const float* prefix_lse, const int32_t* lens,
+                                int32_t max_len, int32_t window, float* weights, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

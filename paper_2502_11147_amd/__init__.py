@@ -27,6 +27,10 @@ EXPORTS = (
     "raas_abi_version", "raas_pool_bytes", "raas_export_state", "raas_set_attention_splits",
     "raas_profile", "raas_profile_read", "raas_prefill_ragged", "raas_decode_step_masked",
     "raas_decode_step_static", "raas_layer_checkpoint_bytes", "raas_save_layer", "raas_load_layer",
+    "raas_create_weight_cache", "raas_destroy_weight_cache", "raas_weight_cache_bytes", "raas_weight_prefill",
+    "raas_weight_step", "raas_weight_export_state", "raas_create_prefix", "raas_destroy_prefix",
+    "raas_prefix_bytes", "raas_prefix_store", "raas_prefix_attention", "raas_prompt_weights_workspace",
+    "raas_prompt_weights",
 )
 
 
@@ -103,6 +107,23 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.raas_profile.restype = i32
     lib.raas_profile_read.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
     lib.raas_profile_read.restype = i32
+    size, fp = ctypes.c_size_t, ctypes.POINTER(ctypes.c_float)
+    for name, restype, *argtypes in (
+            ("raas_create_weight_cache", i32, vp, vp, ctypes.POINTER(vp)),
+            ("raas_destroy_weight_cache", None, vp),
+            ("raas_weight_cache_bytes", size, vp),
+            ("raas_weight_prefill", i32, vp, i32, vp, vp, vp, ip, ip, i32, vp),
+            ("raas_weight_step", i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp),
+            ("raas_weight_export_state", i32, vp, i32, ip, fp, ip, vp),
+            ("raas_create_prefix", i32, vp, vp, ctypes.POINTER(vp)),
+            ("raas_destroy_prefix", None, vp),
+            ("raas_prefix_bytes", size, vp),
+            ("raas_prefix_store", i32, vp, i32, vp, vp, i32, vp),
+            ("raas_prefix_attention", i32, vp, i32, vp, i32, vp, vp, vp),
+            ("raas_prompt_weights_workspace", size, i32, i32, i32, i32, i32),
+            ("raas_prompt_weights", i32, i32, i32, i32, i32, i32, vp, vp, vp, ip, i32, i32, vp, vp, size, vp)):
+        function = getattr(lib, name)
+        function.restype, function.argtypes = restype, argtypes
     _lib = lib
     return lib
 
@@ -303,3 +324,6 @@ class Pool:
         _check(self.lib.raas_profile_read(self._h, kernel, ctypes.byref(ms), ctypes.byref(n)),
                "raas_profile_read")
         return ms.value, n.value
+
+
+from .weight_cache import PrefixConfig, SharedPrefix, WeightCache, WeightConfig, prompt_weights  # noqa: E402,F401

@@ -14,9 +14,13 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libraas.so")
 KERNELS = os.path.join(CSRC, "raas_kernels.hip")
-# translation units of libraas.so: the kernels' file once per RAAS_PART, and the runtime
+# translation units of libraas.so: the kernels' file once per RAAS_PART, the
+# kernels around the weight cache, and the two runtimes
 KERNEL_PARTS = 15
-UNITS = [(KERNELS, ["-DRAAS_PART=%d" % i]) for i in range(KERNEL_PARTS)] + [(os.path.join(CSRC, "raas_runtime.hip"), [])]
+UNITS = [(KERNELS, ["-DRAAS_PART=%d" % i]) for i in range(KERNEL_PARTS)] + [
+    (os.path.join(CSRC, name + ".hip"), [])
+    for name in ("raas_weight_kernels", "raas_prefix_kernels", "raas_prompt_kernels", "raas_runtime",
+                 "raas_weight_runtime")]
 # the streaming probe (measurement only) is a library of its own
 PROBE_SOURCES = [os.path.join(CSRC, "raas_probe.hip")]
 PROBE_LIB_PATH = os.path.join(HERE, "libraas_probe.so")

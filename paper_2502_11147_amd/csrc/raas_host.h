@@ -1,0 +1,15 @@
+// What the host files of the library share: the thread's last error. Not part
+// of the C ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "raas.h"
+
+namespace raas {
+
+// Stores the message that raas_last_error returns and gives `st` back.
+raas_status fail(raas_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+raas_status hip_fail(hipError_t e, const char* what);
+
+}  // namespace raas

@@ -10,10 +10,10 @@
 #include <atomic>
 #include <mutex>
 #include <new>
-#include <string>
 #include <vector>
 
 #include "raas.h"
+#include "raas_host.h"
 #include "raas_internal.h"
 
 using namespace raas;
@@ -41,22 +41,23 @@ bool raas::non_temporal_loads(double own, double others, int units, bool prompt_
 
 namespace {
 
-thread_local std::string g_last_error;
+thread_local char g_last_error[512];
 
-raas_status fail(raas_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-raas_status fail(raas_status st, const char* fmt, ...) {
-    char buf[512];
+}  // namespace
+
+raas_status raas::fail(raas_status st, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
+    vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
     va_end(ap);
-    g_last_error = buf;
     return st;
 }
 
-raas_status hip_fail(hipError_t e, const char* what) {
+raas_status raas::hip_fail(hipError_t e, const char* what) {
     return fail(RAAS_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
 
 constexpr int kKernels = 3;  // step kernel, (none), prompt selection kernel
 constexpr size_t kProfRing = 8192;
@@ -440,7 +441,7 @@ raas_status decode_step(raas_pool* p, int32_t layer, const StepIO& io, hipStream
 
 extern "C" {
 
-const char* raas_last_error(void) { return g_last_error.c_str(); }
+const char* raas_last_error(void) { return g_last_error; }
 
 int32_t raas_abi_version(void) { return RAAS_ABI_VERSION; }
 
