@@ -34,6 +34,9 @@ constexpr int kTokens = 4 * kVec<T>;  // tokens of a block
 template <typename T>
 constexpr int kTiles = kVec<T> / 4;  // 16-token tiles of a block
 
+// This wavefront's number in its workgroup, as a scalar.
+__device__ __forceinline__ int wave_of(int tid) { return __builtin_amdgcn_readfirstlane(tid >> 6); }
+
 __device__ __forceinline__ u32x4 ld16(const void* p) { return *reinterpret_cast<const u32x4*>(p); }
 __device__ __forceinline__ u32x4 ld16_nt(const void* p) {
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_prefix(PrefixView P, const T* _
     constexpr int VE = kVec<T>, BT = kTokens<T>, QT = kTiles<T>, KS = D / (4 * VE), NP = D / 16;
     __shared__ __align__(16) float s_o[kWaves][16][D + 4];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, a = lane >> 4, col = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
     const int h = blockIdx.y, r0 = blockIdx.x * 16 * RT, part = blockIdx.z;
     const int n = *P.len, nb = (n + BT - 1) / BT, per = (nb + P.nsplit - 1) / P.nsplit;
     const int lo = min(nb, part * per), hi = min(nb, lo + per);
@@ -141,7 +141,7 @@ constexpr int kWorkgroups = 512;  // wanted at least
 PrefixPlan plan_prefix(int nkv, int rows, int D, int tokens, bool bf16) {
     const int bt = bf16 ? 32 : 16, nb = (tokens + bt - 1) / bt;
     (void)D;
-    const int want = std::max(1, kWorkgroups / (nkv * row_tiles(rows)));
+    const int want = std::min(kMaxPrefixParts, std::max(1, kWorkgroups / (nkv * row_tiles(rows))));
     return PrefixPlan{std::max(1, std::min(want, (nb + kWaves - 1) / kWaves))};
 }
 

@@ -10,6 +10,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "raas_blocks.h"
 #include "raas_weight_internal.h"
@@ -20,8 +21,11 @@ namespace {
 using namespace blk;
 
 constexpr int kWaves = 4;
-constexpr int kKeys = 16;   // keys of a tile
-constexpr int kRowTiles = 4, kKeyTiles = 4;  // of 16, per wavefront: rows in the first kernel, keys in the second
+constexpr int kThreads = kWaves * 64;
+constexpr int kStage = 64;  // rows (keys of the first kernel, queries of the second) that a workgroup stages in LDS
+// 16-row tiles that a wavefront holds in registers
+template <typename T>
+constexpr int kHeld = sizeof(T) == 2 ? 4 : 2;
 
 __device__ __forceinline__ int seq_rows(const PromptView& v, int len) { return min(len, v.W); }
 // row i * G + g is head g of query i
@@ -34,138 +38,324 @@ __device__ __forceinline__ const T* query_row(const PromptView& v, int b, int h,
     return (const T*)v.q + (((size_t)b * v.W + i) * v.nkv * v.G + (size_t)h * v.G + (row - i * v.G)) * D;
 }
 
-// Grid: row tiles, key chunks, units.
+// kStage rows on their way to LDS: 16-byte pieces, row-major, a piece's place
+// in its row turned by the row's number, so that the 16 rows of an operand's
+// read fall on different banks.
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64) void k_prompt_rows(PromptView v, SeqLens lens) {
-    constexpr int VE = kVec<T>, KS = D / (4 * VE);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, a = lane >> 4, col = lane & 15;
-    const int unit = blockIdx.z, b = v.seq0 + unit / v.nkv, h = unit % v.nkv, chunk = blockIdx.y;
-    const int len = lens.len[unit / v.nkv], nq = seq_rows(v, len), rows = nq * v.G;
-    const int r0 = (blockIdx.x * kWaves + w) * 16 * kRowTiles;
-    if (r0 >= rows) return;
-    u32x4 q[kRowTiles][KS];
-    int last[kRowTiles];  // last key that the row sees
-    float m[kRowTiles], l[kRowTiles];
+struct Staged {
+    static constexpr int NCH = D / kVec<T>, PER = kStage * NCH / kThreads;  // pieces of a row, and of a thread
+    u32x4 x[PER];
+    template <class Row>
+    __device__ __forceinline__ void load(int tid, Row row) {
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t) {
-        const int r = r0 + 16 * t + col, rr = min(r, rows - 1);
+        for (int i = 0; i < PER; ++i) {
+            const int p = tid + i * kThreads;
+            x[i] = ld16_in<T>(row(p / NCH) + (p % NCH) * kVec<T>);
+        }
+    }
+    __device__ __forceinline__ void store(int tid, u32x4* s) const {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = tid + i * kThreads, r = p / NCH;
+            s[r * NCH + ((p % NCH) ^ (r & (NCH - 1)))] = x[i];
+        }
+    }
+    // operand of the 16 rows of tile t
+    __device__ static __forceinline__ void read(const u32x4* s, int t, int a, int col, u32x4 (&o)[D / (4 * kVec<T>)]) {
+        const int r = 16 * t + col;
+#pragma unroll
+        for (int ks = 0; ks < D / (4 * kVec<T>); ++ks) o[ks] = s[r * NCH + ((4 * ks + a) ^ (r & (NCH - 1)))];
+    }
+};
+
+// The log-sum-exp (base 2) of row r of a unit, from its maximum and sum over
+// the prompt's keys; the prefix's joins them.
+__device__ __forceinline__ float row_lse(const PromptView& v, int b, int h, int r, float M, float Z) {
+    if (v.prefix_lse != nullptr) {
+        const int i = query_of(v, r);
+        const float pre = v.prefix_lse[((size_t)b * v.W + i) * v.nkv * v.G + (size_t)h * v.G + (r - i * v.G)] *
+                          1.44269504088896340736f;
+        const float m = fmaxf(M, pre);
+        Z = Z * __builtin_amdgcn_exp2f(M - m) + __builtin_amdgcn_exp2f(pre - m);
+        M = m;
+    }
+    return M + __builtin_amdgcn_logf(Z);
+}
+// A row's maximum and sum over one chunk: its log-sum-exp if there is no other.
+__device__ __forceinline__ void row_done(const PromptView& v, int unit, int b, int h, int r, int chunk, float M,
+                                         float Z) {
+    const size_t at = (size_t)unit * v.W * v.G + r;
+    if (v.chunks == 1) {
+        v.lse[at] = row_lse(v, b, h, r, M, Z);
+    } else {
+        v.ml[2 * (at * v.chunks + chunk)] = M;
+        v.ml[2 * (at * v.chunks + chunk) + 1] = Z;
+    }
+}
+
+// The chunks of a row joined. Grid: rows, units.
+__global__ __launch_bounds__(kThreads) void k_prompt_join(PromptView v, SeqLens lens) {
+    const int unit = blockIdx.y, r = blockIdx.x * kThreads + threadIdx.x, len = lens.len[unit / v.nkv];
+    const int nq = seq_rows(v, len);
+    if (r >= nq * v.G) return;
+    const float* ml = v.ml + 2 * ((size_t)unit * v.W * v.G + r) * v.chunks;
+    const int chunks = (len - nq + query_of(v, r)) / v.chunk_keys + 1;  // those that hold keys for it
+    float M = -INFINITY, Z = 0.0f;
+    for (int c = 0; c < chunks; ++c) M = fmaxf(M, ml[2 * c]);
+    for (int c = 0; c < chunks; ++c) Z += ml[2 * c + 1] * __builtin_amdgcn_exp2f(ml[2 * c] - M);
+    v.lse[(size_t)unit * v.W * v.G + r] = row_lse(v, v.seq0 + unit / v.nkv, unit % v.nkv, r, M, Z);
+}
+
+// Maximum (base 2) and sum of every query row over a chunk of keys. Grid:
+// units, row tiles (the ones that see the most keys first), key chunks: the
+// workgroups that follow each other have equal work, and with eight units each
+// XCD's L2 serves one. ROWS: the
+// wavefronts take RT tiles of 16 rows each and share the staged keys; else (few
+// rows) all take the same RT tiles, and a quarter of the staged keys each.
+template <typename T, int D, int RT, bool ROWS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_rows(PromptView v, SeqLens lens) {
+    constexpr int KS = D / (4 * kVec<T>), SUB = ROWS ? kStage / 16 : kStage / 16 / kWaves;
+    __shared__ __align__(16) u32x4 s_k[kStage * D / kVec<T>];
+    __shared__ float s_m[ROWS ? 1 : kWaves][RT * 16], s_l[ROWS ? 1 : kWaves][RT * 16];
+    const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
+    const int unit = blockIdx.x, b = v.seq0 + unit / v.nkv, h = unit % v.nkv, chunk = blockIdx.z;
+    const int len = lens.len[unit / v.nkv], nq = seq_rows(v, len), rows = nq * v.G;
+    constexpr int WG_ROWS = 16 * RT * (ROWS ? kWaves : 1);
+    const int wg0 = (gridDim.y - 1 - blockIdx.y) * WG_ROWS;
+    if (wg0 >= rows) return;
+    const int r0 = wg0 + (ROWS ? w * 16 * RT : 0), lo = chunk * v.chunk_keys;
+    // keys that the workgroup's and this wavefront's last row see
+    const int seen = len - nq + query_of(v, min(wg0 + WG_ROWS, rows) - 1) + 1, hi = min(seen, lo + v.chunk_keys);
+    if (lo >= hi) return;
+    const int mine = r0 < rows ? min(hi, len - nq + query_of(v, min(r0 + 16 * RT, rows) - 1) + 1) : 0;
+    const int full = len - nq + query_of(v, min(r0, rows - 1));  // last key that every row of the wavefront sees
+    u32x4 q[RT][KS];
+    int last[RT];  // last key that the row sees
+    float m[RT], l[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int rr = min(r0 + 16 * t + col, rows - 1);
         load_row<T, D>(query_row<T, D>(v, b, h, rr), true, a, q[t]);
         last[t] = len - nq + query_of(v, rr);
         m[t] = -INFINITY;
         l[t] = 0.0f;
     }
-    const int seen = len - nq + query_of(v, min(r0 + 16 * kRowTiles, rows) - 1) + 1;
-    const int hi = min(seen, (chunk + 1) * v.chunk_keys);
     const T* K = (const T*)v.k + ((size_t)b * v.nkv + h) * v.P * D;
-    for (int j0 = chunk * v.chunk_keys; j0 < hi; j0 += kKeys) {
-        u32x4 k[KS];
-        load_row<T, D>(K + (size_t)min(j0 + col, len - 1) * D, true, a, k);
+    Staged<T, D> next;
+    next.load(tid, [&](int r) { return K + (size_t)min(lo + r, len - 1) * D; });
+    for (int j0 = lo; j0 < hi; j0 += kStage) {
+        __syncthreads();
+        next.store(tid, s_k);
+        __syncthreads();
+        if (j0 + kStage < hi) next.load(tid, [&](int r) { return K + (size_t)min(j0 + kStage + r, len - 1) * D; });
+        if (j0 >= mine) continue;
+        const int jw = j0 + (ROWS ? 0 : w * 16 * SUB);
+        auto stage = [&](auto masked) {
+            f32x4 x[RT][SUB];
 #pragma unroll
-        for (int t = 0; t < kRowTiles; ++t) {
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) x = mfma16<T>(k[ks], q[t][ks], x);
-            float mb = -INFINITY;
+                for (int c = 0; c < SUB; ++c) x[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = j0 + 4 * a + r <= last[t] ? x[r] * v.scale_log2 : -INFINITY;
-                mb = fmaxf(mb, x[r]);
+            for (int c = 0; c < SUB; ++c) {
+                u32x4 k[KS];
+                Staged<T, D>::read(s_k, ROWS ? c : w * SUB + c, a, col, k);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) x[t][c] = mfma16<T>(k[ks], q[t][ks], x[t][c]);
             }
-            const float mn = fmaxf(m[t], mb), ref = mn == -INFINITY ? 0.0f : mn;
-            l[t] *= __builtin_amdgcn_exp2f(m[t] - ref);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) l[t] += __builtin_amdgcn_exp2f(x[r] - ref);
-            m[t] = mn;
-        }
+            for (int t = 0; t < RT; ++t) {
+                if constexpr (masked) {
+#pragma unroll
+                    for (int c = 0; c < SUB; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[t][c][e] = jw + 16 * c + 4 * a + e <= last[t] ? x[t][c][e] : -INFINITY;
+                }
+                float mb = x[t][0][0];
+#pragma unroll
+                for (int c = 0; c < SUB; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mb = fmaxf(mb, x[t][c][e]);
+                const float mn = fmaxf(m[t], mb * v.scale_log2), ref = mn == -INFINITY ? 0.0f : mn;
+                float add = 0.0f;
+#pragma unroll
+                for (int c = 0; c < SUB; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        add += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][c][e], v.scale_log2, -ref));
+                l[t] = __builtin_fmaf(l[t], __builtin_amdgcn_exp2f(m[t] - ref), add);
+                m[t] = mn;
+            }
+        };
+        // (two bodies: a branch inside would keep products and exponentials apart)
+        if (jw + 16 * SUB - 1 > full) stage(std::true_type{});
+        else stage(std::false_type{});
     }
 #pragma unroll
-    for (int t = 0; t < kRowTiles; ++t) {
-        const float M = max_groups(m[t]), ref = M == -INFINITY ? 0.0f : M;
-        const float Z = sum_groups(l[t] * __builtin_amdgcn_exp2f(m[t] - ref));
-        const int r = r0 + 16 * t + col;
-        if (a == 0 && r < rows) {
-            float* to = v.ml + 2 * (((size_t)unit * v.W * v.G + r) * v.chunks + chunk);
-            to[0] = M;
-            to[1] = Z;
+    for (int t = 0; t < RT; ++t) {
+        float M = max_groups(m[t]);
+        float ref = M == -INFINITY ? 0.0f : M;
+        float Z = sum_groups(l[t] * __builtin_amdgcn_exp2f(m[t] - ref));
+        if constexpr (!ROWS) {
+            if (a == 0) {
+                s_m[w][16 * t + col] = M;
+                s_l[w][16 * t + col] = Z;
+            }
+        } else {
+            const int r = r0 + 16 * t + col;
+            if (a == 0 && r < rows) row_done(v, unit, b, h, r, chunk, M, Z);
+        }
+    }
+    if constexpr (!ROWS) {
+        __syncthreads();
+        const int r = r0 + tid;
+        if (tid < RT * 16 && r < rows) {
+            float M = -INFINITY, Z = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) M = fmaxf(M, s_m[i][tid]);
+            const float ref = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) Z += s_l[i][tid] * __builtin_amdgcn_exp2f(s_m[i][tid] - ref);
+            row_done(v, unit, b, h, r, chunk, M, Z);
         }
     }
 }
 
-// Grid: key tiles of a workgroup, units.
+// Probabilities of a chunk of query rows, summed per key. Grid: units, key
+// tiles (the ones that most rows see first), row chunks. A wavefront holds kHeld
+// tiles of 16 keys; the rows pass through LDS with their log-sum-exp (base 2).
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64) void k_prompt_keys(PromptView v, SeqLens lens) {
-    constexpr int VE = kVec<T>, KS = D / (4 * VE);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, a = lane >> 4, col = lane & 15;
-    const int unit = blockIdx.y, b = v.seq0 + unit / v.nkv, h = unit % v.nkv;
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_keys(PromptView v, SeqLens lens) {
+    constexpr int KS = D / (4 * kVec<T>), KT = kHeld<T>, SUB = kStage / 16;
+    __shared__ __align__(16) u32x4 s_q[kStage * D / kVec<T>];
+    __shared__ float s_lse[kStage];
+    const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
+    const int unit = blockIdx.x, b = v.seq0 + unit / v.nkv, h = unit % v.nkv;
     const int len = lens.len[unit / v.nkv], nq = seq_rows(v, len), rows = nq * v.G;
-    const int j0 = (blockIdx.x * kWaves + w) * 16 * kKeyTiles;
-    if (j0 >= len) return;
+    const int wg0 = blockIdx.y * kWaves * 16 * KT, j0 = wg0 + w * 16 * KT;
+    if (wg0 >= len) return;
     const T* K = (const T*)v.k + ((size_t)b * v.nkv + h) * v.P * D;
-    u32x4 k[kKeyTiles][KS];
-    f32x4 sum[kKeyTiles];
+    u32x4 k[KT][KS];
+    f32x4 sum[KT];
 #pragma unroll
-    for (int t = 0; t < kKeyTiles; ++t) {
+    for (int t = 0; t < KT; ++t) {
         load_row<T, D>(K + (size_t)min(j0 + 16 * t + col, len - 1) * D, true, a, k[t]);
         sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // the first query that sees this tile's first key
-    const int first = max(0, j0 - (len - nq)) * v.G;
-    for (int r0 = first & ~15; r0 < rows; r0 += 16) {
-        const int r = r0 + col, rr = min(r, rows - 1);
-        u32x4 q[KS];
-        load_row<T, D>(query_row<T, D>(v, b, h, rr), true, a, q);
-        const int i = query_of(v, rr);
-        const float* ml = v.ml + 2 * ((size_t)unit * v.W * v.G + rr) * v.chunks;
-        float M = -INFINITY, Z = 0.0f, pre = -INFINITY;
-        if (v.prefix_lse != nullptr)
-            pre = v.prefix_lse[((size_t)b * v.W + i) * v.nkv * v.G + (size_t)h * v.G + (rr - i * v.G)] *
-                  1.44269504088896340736f;
-        M = pre;
-        for (int c = 0; c < v.chunks; ++c) M = fmaxf(M, ml[2 * c]);
-        if (pre != -INFINITY) Z = __builtin_amdgcn_exp2f(pre - M);
-        for (int c = 0; c < v.chunks; ++c) Z += ml[2 * c + 1] * __builtin_amdgcn_exp2f(ml[2 * c] - M);
-        const float lse = M + __builtin_amdgcn_logf(Z);
-        const int last = r < rows ? len - nq + i : -1;
+    // the first rows that see the workgroup's and this wavefront's first key
+    const int first = max(0, wg0 - (len - nq)) * v.G, mine = max(0, j0 - (len - nq)) * v.G;
+    const int lo = blockIdx.z * v.chunk_rows, hi = min(rows, lo + v.chunk_rows);
+    Staged<T, D> next;
+    float lse = 0.0f;
+    auto load = [&](int r0) {
+        next.load(tid, [&](int r) { return query_row<T, D>(v, b, h, min(r0 + r, rows - 1)); });
+        if (tid >= kStage) return;
+        // (rows behind the last weigh nothing)
+        lse = r0 + tid < rows ? v.lse[(size_t)unit * v.W * v.G + r0 + tid] : INFINITY;
+    };
+    const int start = max(lo, first) / kStage * kStage;
+    if (start < hi) load(start);
+    for (int r0 = start; r0 < hi; r0 += kStage) {
+        __syncthreads();
+        next.store(tid, s_q);
+        if (tid < kStage) s_lse[tid] = lse;
+        __syncthreads();
+        if (r0 + kStage < hi) load(r0 + kStage);
+        if (r0 + kStage <= mine || j0 >= len) continue;
+        // (two bodies: a branch inside would keep products and exponentials apart)
+        auto stage = [&](auto masked) {
 #pragma unroll
-        for (int t = 0; t < kKeyTiles; ++t) {
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            for (int c = 0; c < SUB; ++c) {
+                u32x4 q[KS];
+                Staged<T, D>::read(s_q, c, a, col, q);
+                const float off = s_lse[16 * c + col];
+                const int last = masked ? len - nq + query_of(v, r0 + 16 * c + col) : 0;
+                f32x4 x[KT];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) x = mfma16<T>(k[t][ks], q[ks], x);
+                for (int t = 0; t < KT; ++t) x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                sum[t][e] += j0 + 16 * t + 4 * a + e <= last
-                                 ? __builtin_amdgcn_exp2f(x[e] * v.scale_log2 - lse) : 0.0f;
-        }
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) x[t] = mfma16<T>(k[t][ks], q[ks], x[t]);
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = __builtin_fmaf(x[t][e], v.scale_log2, -off);
+                        sum[t][e] +=
+                            __builtin_amdgcn_exp2f(masked && j0 + 16 * t + 4 * a + e > last ? -INFINITY : y);
+                    }
+            }
+        };
+        if (len - nq + query_of(v, r0) < j0 + 16 * KT - 1) stage(std::true_type{});
+        else stage(std::false_type{});
     }
+    float* to = v.row_chunks == 1 ? v.weights + ((size_t)b * v.nkv + h) * v.P
+                                  : v.part + ((size_t)blockIdx.z * v.nseq * v.nkv + unit) * v.P;
 #pragma unroll
-    for (int t = 0; t < kKeyTiles; ++t)
+    for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float x = sum[t][e];
 #pragma unroll
             for (int d = 8; d >= 1; d >>= 1) x += __shfl_xor(x, d);
             const int j = j0 + 16 * t + 4 * a + e;
-            if (col == 0 && j < len) v.weights[((size_t)b * v.nkv + h) * v.P + j] = x;
+            if (col == 0 && j < len) to[j] = x;
         }
+}
+
+// The row chunks' sums, added up. Grid: keys, units.
+__global__ __launch_bounds__(kThreads) void k_prompt_sum(PromptView v, SeqLens lens) {
+    const int unit = blockIdx.y, j = blockIdx.x * kThreads + threadIdx.x;
+    if (j >= lens.len[unit / v.nkv]) return;
+    float x = 0.0f;
+    for (int c = 0; c < v.row_chunks; ++c) x += v.part[((size_t)c * v.nseq * v.nkv + unit) * v.P + j];
+    v.weights[((size_t)v.seq0 * v.nkv + unit) * v.P + j] = x;
 }
 
 template <typename T, int D>
 void launch_t(const PromptView& v, const SeqLens& lens, int most, hipStream_t s) {
     const int units = v.nseq * v.nkv, rows = std::min(most, v.W) * v.G;
-    const int row_step = kWaves * 16 * kRowTiles, key_step = kWaves * 16 * kKeyTiles;
-    hipLaunchKernelGGL((k_prompt_rows<T, D>), dim3((rows + row_step - 1) / row_step, v.chunks, units),
-                       dim3(kWaves * 64), 0, s, v, lens);
-    hipLaunchKernelGGL((k_prompt_keys<T, D>), dim3((most + key_step - 1) / key_step, units), dim3(kWaves * 64), 0, s,
-                       v, lens);
+    const int chunks = (most + v.chunk_keys - 1) / v.chunk_keys, key_step = kWaves * 16 * kHeld<T>;
+    auto go = [&](auto kernel, int step) {
+        hipLaunchKernelGGL(kernel, dim3(units, (rows + step - 1) / step, chunks), dim3(kThreads), 0, s, v, lens);
+    };
+    if (rows <= 16) go(k_prompt_rows<T, D, 1, false>, 16);
+    else if (rows <= 16 * kHeld<T>) go(k_prompt_rows<T, D, kHeld<T>, false>, 16 * kHeld<T>);
+    else go(k_prompt_rows<T, D, kHeld<T>, true>, 16 * kHeld<T> * kWaves);
+    if (v.chunks > 1)
+        hipLaunchKernelGGL(k_prompt_join, dim3((rows + kThreads - 1) / kThreads, units), dim3(kThreads), 0, s, v, lens);
+    hipLaunchKernelGGL((k_prompt_keys<T, D>), dim3(units, (most + key_step - 1) / key_step, v.row_chunks),
+                       dim3(kThreads), 0, s, v, lens);
+    if (v.row_chunks > 1)
+        hipLaunchKernelGGL(k_prompt_sum, dim3((most + kThreads - 1) / kThreads, units), dim3(kThreads), 0, s, v, lens);
 }
 
 }  // namespace
 
-int plan_prompt_chunks(int units, int G, int W, int P) {
-    const int row_step = kWaves * 16 * kRowTiles;
-    const long long wgs = (long long)units * (((long long)W * G + row_step - 1) / row_step);
-    const int want = (int)std::max<long long>(1, std::min<long long>(16, 512 / std::max<long long>(1, wgs)));
-    return std::max(1, std::min(want, P / 256));
+// Workgroups wanted in each of the two kernels: about six per CU, so that the
+// causal part's uneven ones even out.
+constexpr int kWorkgroups = 1536;
+
+PromptPlan plan_prompt(int units, int G, int W, int P, bool bf16) {
+    const int held = bf16 ? kHeld<uint16_t> : kHeld<float>;
+    const long long rows = (long long)W * G, row_step = rows <= 16 ? 16 : 16LL * held * (rows <= 16 * held ? 1 : kWaves);
+    const long long row_wgs = units * ((rows + row_step - 1) / row_step);
+    const long long key_wgs = units * (((long long)P + kWaves * 16 * held - 1) / (kWaves * 16 * held));
+    PromptPlan p;
+    // at least 512 keys or rows a piece
+    const long long want = std::min<long long>(kWorkgroups / row_wgs, P / 512);
+    p.chunks = (int)std::max<long long>(1, want);
+    p.chunk_keys = (int)(((P + p.chunks - 1) / p.chunks + kStage - 1) / kStage * kStage);
+    p.chunks = (P + p.chunk_keys - 1) / p.chunk_keys;
+    const long long want_rows = std::min<long long>(kWorkgroups / key_wgs, rows / 512);
+    p.row_chunks = (int)std::max<long long>(1, want_rows);
+    p.chunk_rows = (int)(((rows + p.row_chunks - 1) / p.row_chunks + kStage - 1) / kStage * kStage);
+    p.row_chunks = (int)((rows + p.chunk_rows - 1) / p.chunk_rows);
+    return p;
 }
 
 hipError_t launch_prompt_weights(const PromptView& v, bool bf16, const SeqLens& lens, hipStream_t s) {

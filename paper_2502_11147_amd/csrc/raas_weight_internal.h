@@ -26,13 +26,15 @@ struct SeqLens {
 struct WeightView {
     void* K;       // [U][cpad][D] in blocks (raas_blocks.h)
     void* V;       // [U][cpad][D] likewise
-    int32_t* pos;  // [U][C] absolute position, -1 when free
-    float* w;      // [U][C] accumulated weight
+    int32_t* pos;  // [U][cpad] absolute position, -1 when free
+    float* w;      // [U][cpad] accumulated weight
     int32_t* unit; // [U][kWeightFields]
     float* logits; // [U][G][cpad] scratch of one step of split units
     float* part;   // [U][nsplit][G][D] unnormalised outputs of the splits, likewise
     float* ml;     // [U][nsplit][G][2] their maxima (base 2) and sums
+    int32_t* arrived;  // [U] splits of the unit that have published; zero between launches
     int U, G, D, C, cpad, nkv, recent, nsplit;
+    int wfloats;   // LDS floats of the parts' shares
     float scale_log2;
 };
 
@@ -43,6 +45,7 @@ struct PrefixParts {
     const float* ml;  // [n][nkv * rows][2]
     int n, rows;
 };
+constexpr int kMaxPrefixParts = 64;
 
 struct WeightStepIO {
     const void* q;
@@ -56,15 +59,17 @@ struct WeightStepIO {
     PrefixParts prefix;  // n = 0: none
 };
 
+// Most workgroups that a unit of the step is split over.
+constexpr int kMaxStepSplits = 64;
 struct WeightPlan {
-    int waves;   // wavefronts per workgroup of the step kernel
-    int nsplit;  // workgroups per unit
-    bool fused;  // one workgroup per unit, which finishes the step itself
-    size_t lds;  // dynamic LDS of the step kernel
+    int waves;    // wavefronts per workgroup
+    int nsplit;   // workgroups per unit
+    bool fused;   // one workgroup per unit, which keeps the logits in LDS
+    bool stream;  // keys and values are read with non-temporal loads
 };
-WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16);
-
-hipError_t weight_allow_lds(bool bf16, int D);
+// layer_bytes: keys and values of the layers that are stepped in turn
+WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16, double layer_bytes);
+hipError_t weight_allow_lds(bool bf16, int D, int waves);
 // Chooses the kept tokens of each selected unit and writes its records, then
 // stores their keys and values. Sequences seq0 .. seq0 + nseq - 1.
 hipError_t launch_weight_prefill(const WeightView& L, bool bf16, const void* k, const void* v, const float* weights,
@@ -95,25 +100,31 @@ hipError_t launch_prefix_store(void* K, void* V, int32_t* len, int nkv, int D, i
 hipError_t launch_prefix_attention(const PrefixView& P, bool bf16, const void* q, hipStream_t s);
 hipError_t launch_prefix_join(const PrefixView& P, bool bf16, void* out, float* lse, hipStream_t s);
 
-// Keys and values of `units` units to blocks: row t of unit u comes from row
-// pos[u * C + t] of its source (pos NULL: row t), for t < min(len, C).
+// Keys and values of units to blocks: row t of unit u comes from row
+// pos[u * pad + t] of its source (pos NULL: row t), for t < min(len, C).
 struct StoreIn {
     const int32_t* pos;
     int C, pad, nkv, seq0, stride, tokens;  // tokens >= 0: every unit's length; else lens
 };
 
 // Weights of prompts (raas_prompt_weights): sequences seq0 .. seq0 + nseq - 1.
-struct PromptView {
+struct PromptPlan {
+    int chunks, chunk_keys;      // pieces of the keys in the pass that finds the rows' sums
+    int row_chunks, chunk_rows;  // pieces of the rows in the pass that adds up their probabilities
+};
+PromptPlan plan_prompt(int units, int G, int W, int P, bool bf16);
+struct PromptView : PromptPlan {
     const void* q;           // [B][W][Hq][D]
     const void* k;           // [B][nkv][P][D]
     const float* prefix_lse; // [B][W][Hq] or NULL
     float* weights;          // [B][nkv][P]
-    float* ml;               // [nseq * nkv][W * G][chunks][2] scratch
-    int W, P, G, D, nkv, seq0, nseq, chunks, chunk_keys;
+    float* lse;              // [nseq * nkv][W * G] scratch: each row's log-sum-exp (base 2)
+    float* ml;               // [nseq * nkv][W * G][chunks][2] scratch, if chunks > 1: maxima and sums
+    float* part;             // [row_chunks][nseq * nkv][P] scratch, if row_chunks > 1
+    int W, P, G, D, nkv, seq0, nseq;
     uint32_t g_magic;        // row / G = umulhi(row, g_magic), G > 1
     float scale_log2;
 };
-int plan_prompt_chunks(int units, int G, int W, int P);
 hipError_t launch_prompt_weights(const PromptView& v, bool bf16, const SeqLens& lens, hipStream_t s);
 
 }  // namespace raas

@@ -13,6 +13,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "raas_blocks.h"
 #include "raas_weight_internal.h"
@@ -23,7 +24,7 @@ namespace {
 using namespace blk;
 
 // Bytes of dynamic LDS that a step workgroup may use (gfx950 has 160 KiB).
-constexpr size_t kStepLds = 144 * 1024;
+constexpr size_t kStepLds = 156 * 1024;
 
 // ---------------------------------------------------------------------------
 // The lightest token: least (weight, position), with its place.
@@ -106,8 +107,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_weight_select(WeightView L, 
     if (P < 0) return;  // not selected
     const int u = seq0 * L.nkv + blockIdx.x, C = L.C;
     const float* wu = weights + (size_t)u * max_len;
-    int32_t* pos = L.pos + (size_t)u * C;
-    float* w = L.w + (size_t)u * C;
+    int32_t* pos = L.pos + (size_t)u * L.cpad;
+    float* w = L.w + (size_t)u * L.cpad;
     // (+ 0 turns -0 into 0, which would otherwise rank below it)
     auto weight = [&](int j) { return weights != nullptr ? wu[j] + 0.0f : 0.0f; };
     const int first = max(P - L.recent, 0);  // tokens before it may go
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256) void k_store(T* __restrict__ K, T* __restrict_
     const u32x4 zero = {0u, 0u, 0u, 0u};
     for (int b = blockIdx.y; b * BT < n; b += gridDim.y) {
         const int t0 = b * BT, valid = min(BT, n - t0);
-        auto row = [&](int t) { return (size_t)(in.pos != nullptr ? in.pos[(size_t)u * in.C + t0 + t] : t0 + t) * D; };
+        auto row = [&](int t) { return (size_t)(in.pos != nullptr ? in.pos[(size_t)u * in.pad + t0 + t] : t0 + t) * D; };
         T* Kb = K + ((size_t)u * in.pad + t0) * D;
         T* Vb = V + ((size_t)u * in.pad + t0) * D;
         for (int p = tid; p < BT * RP; p += 256) {
@@ -212,59 +213,151 @@ __global__ __launch_bounds__(256) void k_store(T* __restrict__ K, T* __restrict_
 __global__ void k_set_int(int32_t* p, int32_t v) { *p = v; }
 
 // ---------------------------------------------------------------------------
+// Hand-over between workgroups of one launch. The XCDs' L2s are not coherent
+// with each other, so what crosses is written through and read past them (agent
+// scope); once a wavefront's stores are acknowledged every XCD reads them.
+template <typename T>
+__device__ __forceinline__ void publish(T* p, T v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T published(const T* p) {
+    return __hip_atomic_load(const_cast<T*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void publish4(float* p, f32x4 v) {  // p: 16-byte aligned
+    unsigned long long* q = reinterpret_cast<unsigned long long*>(p);
+    publish(q, (unsigned long long)__float_as_uint(v[1]) << 32 | __float_as_uint(v[0]));
+    publish(q + 1, (unsigned long long)__float_as_uint(v[3]) << 32 | __float_as_uint(v[2]));
+}
+__device__ __forceinline__ f32x4 published4(const float* p) {
+    const unsigned long long* q = reinterpret_cast<const unsigned long long*>(p);
+    const unsigned long long x = published(q), y = published(q + 1);
+    return f32x4{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)), __uint_as_float((uint32_t)y),
+                 __uint_as_float((uint32_t)(y >> 32))};
+}
+// True on the last of `total` workgroups to call it for this counter, once all
+// that they published is readable; the counter is zero again afterwards. No
+// workgroup waits for another.
+__device__ __forceinline__ bool arrive_last(int32_t* counter, int total) {
+    __shared__ int s_last;
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == total - 1) publish(counter, 0);
+        s_last = before == total - 1;
+    }
+    __syncthreads();
+    return s_last != 0;
+}
+
+// ---------------------------------------------------------------------------
 // The end of a step: from the maxima and sums (ml) and unnormalised outputs (o)
 // of `nsrc` disjoint parts of the held tokens, and those of the prefix, the
-// output; from the logits the weights; the new token's position; the lightest
-// token. One workgroup of NT threads.
-template <typename T, int D, int NT, class Ml, class O>
+// output; from the logits (x4: those of four tokens) the weights; the new
+// token's position; the lightest token. One workgroup of NW wavefronts; s_w:
+// [nsrc + prefix parts][G] floats of LDS. A wavefront per head finds the
+// maximum and the sum, a lane per part; a thread takes four tokens at a time.
+typedef int32_t i32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T, int D, int NW, class Ml, class O, class X4>
 __device__ __forceinline__ void finish_step(const WeightView& L, const WeightStepIO& io, int u, const int4& rec,
-                                            const float* logits, int lstride, int nsrc, Ml ml, O o) {
+                                            int nsrc, float* s_w, Ml ml, O o, X4 x4) {
+    constexpr int NT = NW * 64, STEP = NT * 4;
     __shared__ float s_m[16], s_rz[16];
-    const int tid = threadIdx.x, G = L.G, C = L.C;
+    const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), G = L.G, C = L.C;
     const PrefixParts& pp = io.prefix;
     const size_t rows = (size_t)L.nkv * pp.rows, row0 = (size_t)(u % L.nkv) * pp.rows + (size_t)(u / L.nkv) * G;
-    if (tid < G) {
+    const int now = rec.y, place = rec.z, n = min(rec.x + 1, C), before = now + 1 - L.recent;
+    int32_t* pos = L.pos + (size_t)u * L.cpad;
+    float* wt = L.w + (size_t)u * L.cpad;
+    // the first tokens' records travel while the parts are joined
+    i32x4 p4 = {0, 0, 0, 0};
+    f32x4 w4 = {0.f, 0.f, 0.f, 0.f};
+    if (4 * tid < n) {
+        p4 = *reinterpret_cast<const i32x4*>(pos + 4 * tid);
+        w4 = *reinterpret_cast<const f32x4*>(wt + 4 * tid);
+    }
+    const int parts = nsrc + pp.n;
+    for (int g = w; g < G; g += NW) {
+        auto part_ml = [&](int s) {
+            if (s < nsrc) return ml(s, g);
+            const float* x = pp.ml + 2 * ((size_t)(s - nsrc) * rows + row0 + g);
+            return make_float2(x[0], x[1]);
+        };
         float M = -INFINITY, Z = 0.0f;
-        for (int s = 0; s < nsrc; ++s) M = fmaxf(M, ml(s, tid).x);
-        for (int s = 0; s < pp.n; ++s) M = fmaxf(M, pp.ml[2 * (s * rows + row0 + tid)]);
-        for (int s = 0; s < nsrc; ++s) Z += ml(s, tid).y * __builtin_amdgcn_exp2f(ml(s, tid).x - M);
-        for (int s = 0; s < pp.n; ++s) {
-            const float* x = pp.ml + 2 * (s * rows + row0 + tid);
-            Z += x[1] * __builtin_amdgcn_exp2f(x[0] - M);
+        const float2 first = lane < parts ? part_ml(lane) : make_float2(-INFINITY, 0.0f);
+        M = first.x;
+        for (int s = lane + 64; s < parts; s += 64) M = fmaxf(M, part_ml(s).x);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+        Z = first.y * __builtin_amdgcn_exp2f(first.x - M);
+        for (int s = lane + 64; s < parts; s += 64) {
+            const float2 y = part_ml(s);
+            Z += y.y * __builtin_amdgcn_exp2f(y.x - M);
         }
-        s_m[tid] = M;
-        s_rz[tid] = 1.0f / Z;
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) Z += __shfl_xor(Z, d);
+        const float rz = 1.0f / Z;
+        if (lane < parts) s_w[lane * G + g] = __builtin_amdgcn_exp2f(first.x - M) * rz;
+        for (int s = lane + 64; s < parts; s += 64) s_w[s * G + g] = __builtin_amdgcn_exp2f(part_ml(s).x - M) * rz;
+        if (lane == 0) {
+            s_m[g] = M;
+            s_rz[g] = rz;
+        }
     }
     __syncthreads();
     for (int i = tid; i < G * D; i += NT) {
         const int g = i / D, c = i % D;
-        const float M = s_m[g];
         float x = 0.0f;
-        for (int s = 0; s < nsrc; ++s) x += o(s, g, c) * __builtin_amdgcn_exp2f(ml(s, g).x - M);
-        for (int s = 0; s < pp.n; ++s)
-            x += pp.o[(s * rows + row0 + g) * D + c] *
-                 __builtin_amdgcn_exp2f(pp.ml[2 * (s * rows + row0 + g)] - M);
-        ((T*)io.out)[((size_t)u * G + g) * D + c] = from_f<T>(x * s_rz[g]);
+#pragma unroll 8
+        for (int s = 0; s < nsrc; ++s) x += o(s, g, c) * s_w[s * G + g];
+#pragma unroll 8
+        for (int s = 0; s < pp.n; ++s) x += pp.o[(s * rows + row0 + g) * D + c] * s_w[(nsrc + s) * G + g];
+        ((T*)io.out)[((size_t)u * G + g) * D + c] = from_f<T>(x);
     }
-    const int now = rec.y, place = rec.z, n = min(rec.x + 1, C), before = now + 1 - L.recent;
-    int32_t* pos = L.pos + (size_t)u * C;
-    float* w = L.w + (size_t)u * C;
     Lightest best;
-    for (int j = tid; j < n; j += NT) {
-        float a = 0.0f;
-        for (int g = 0; g < G; ++g)
-            a += __builtin_amdgcn_exp2f(logits[(size_t)g * lstride + j] - s_m[g]) * s_rz[g];
-        const int p = j == place ? now : pos[j];
-        const float x = (j == place ? 0.0f : w[j]) + a;
-        if (j == place) pos[j] = now;
-        w[j] = x;
-        if (io.positions_out) io.positions_out[(size_t)u * C + j] = p;
-        if (io.weights_out) io.weights_out[(size_t)u * C + j] = x;
-        if (p < before) best.offer(x, p, j);
-    }
-    for (int j = n + tid; j < C; j += NT) {
-        if (io.positions_out) io.positions_out[(size_t)u * C + j] = -1;
-        if (io.weights_out) io.weights_out[(size_t)u * C + j] = 0.0f;
+    for (int j = 4 * tid; j < C; j += STEP) {
+        if (j >= n && io.positions_out == nullptr && io.weights_out == nullptr) break;
+        if (j > 4 * tid && j < n) {
+            p4 = *reinterpret_cast<const i32x4*>(pos + j);
+            w4 = *reinterpret_cast<const f32x4*>(wt + j);
+        }
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        if (j < n) {
+#pragma unroll 4
+            for (int g = 0; g < G; ++g) {
+                const f32x4 x = x4(g, j);
+                const float M = s_m[g], rz = s_rz[g];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - M), rz, a[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool fresh = j + e == place, held = j + e < n;
+            p4[e] = fresh ? now : held ? p4[e] : -1;
+            w4[e] = held ? (fresh ? 0.0f : w4[e]) + a[e] : 0.0f;
+            if (held && p4[e] < before) best.offer(w4[e], p4[e], j + e);
+        }
+        if (j < n) {
+            *reinterpret_cast<f32x4*>(wt + j) = w4;
+            if (place >= j && place < j + 4) pos[place] = now;
+        }
+        if (j + 4 <= C) {
+            if (io.positions_out) *reinterpret_cast<i32x4_at4*>(io.positions_out + (size_t)u * C + j) = p4;
+            if (io.weights_out) *reinterpret_cast<f32x4_at4*>(io.weights_out + (size_t)u * C + j) = w4;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (j + e < C) {
+                    if (io.positions_out) io.positions_out[(size_t)u * C + j + e] = p4[e];
+                    if (io.weights_out) io.weights_out[(size_t)u * C + j + e] = w4[e];
+                }
+        }
     }
     if (n == C) best = lightest_wg<NT>(best, tid);
     if (tid == 0) {
@@ -274,44 +367,54 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
 }
 
 // ---------------------------------------------------------------------------
-// The step: one workgroup of NW wavefronts per (unit, split). A wavefront takes
-// every NW-th block of its split, so the order of every sum is fixed; a block
+// The step: one workgroup of NW wavefronts per (unit, split). Split s of a unit
+// takes every nsplit-th block, a wavefront every NW-th of those, so the order of
+// every sum is fixed and the work is even however many tokens are held; a block
 // is read while the one before it is attended to. The new token's row is
 // replaced in registers by the wavefront that holds its block, which stores it.
-template <typename T, int D, int NW, bool FUSED>
+// FUSED: one workgroup covers the unit and keeps the logits in LDS; else the
+// last of the unit's workgroups to end finishes the step from what all of them
+// published. STREAM: the layer does not stay in the memory-side cache.
+template <typename T, int D, int NW, bool FUSED, bool STREAM>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_weight_step(WeightView L,
                                                                                                  WeightStepIO io) {
     constexpr int VE = kVec<T>, BT = kTokens<T>, QT = kTiles<T>, KS = D / (4 * VE), NP = D / 16;
     extern __shared__ __align__(16) float smem[];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, a = lane >> 4, col = lane & 15;
-    const int u = blockIdx.x / L.nsplit, split = blockIdx.x - u * L.nsplit;
+    const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
+    const int u = FUSED ? blockIdx.x : blockIdx.x / L.nsplit, split = FUSED ? 0 : blockIdx.x - u * L.nsplit;
+    const int nsplit = FUSED ? 1 : L.nsplit;
     if (io.active != nullptr && io.active[u / L.nkv] == 0) return;  // the sequence sits this step out
     const int G = L.G;
     float* s_ml = smem;                    // [NW][16][2]
-    float* s_o = s_ml + NW * 32;           // [NW][G][D + 4]
+    float* s_w = s_ml + NW * 32;           // [parts][G], 16-byte multiple
+    float* s_o = s_w + L.wfloats;          // [NW][G][D + 4]
     float* s_x = s_o + NW * G * (D + 4);   // [G][cpad], fused only
-    const int4 rec = *reinterpret_cast<const int4*>(L.unit + (size_t)u * kWeightFields);
-    const int n = min(rec.x + 1, L.C), nb = (n + BT - 1) / BT, per = (nb + L.nsplit - 1) / L.nsplit;
-    const int lo = min(nb, split * per), hi = min(nb, lo + per);
-    const int tail = rec.z / BT;  // the block that the new token goes to
     T* Ku = (T*)L.K + (size_t)u * L.cpad * D;
     T* Vu = (T*)L.V + (size_t)u * L.cpad * D;
+    const int last_block = L.cpad / BT - 1, step = NW * nsplit;
+
+    u32x4 k0[NP], v0[NP], k1[NP], v1[NP];
+    auto load = [&](int b, u32x4 (&kr)[NP], u32x4 (&vr)[NP]) {
+        const size_t at = (size_t)min(b, last_block) * BT * D + lane * VE;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) kr[i] = STREAM ? ld16_nt(Ku + at + i * 64 * VE) : ld16(Ku + at + i * 64 * VE);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) vr[i] = STREAM ? ld16_nt(Vu + at + i * 64 * VE) : ld16(Vu + at + i * 64 * VE);
+    };
+    // (the first block's place does not depend on the record, which arrives meanwhile)
+    int b = split + nsplit * w;
+    load(b, k0, v0);
+    const int4 rec = *reinterpret_cast<const int4*>(L.unit + (size_t)u * kWeightFields);
     const T* kn = (const T*)io.k_new + (size_t)u * D;
     const T* vn = (const T*)io.v_new + (size_t)u * D;
-    float* xs = FUSED ? s_x : L.logits + (size_t)u * G * L.cpad;
-
     u32x4 q[KS];
     load_row<T, D>((const T*)io.q + ((size_t)u * G + col) * D, col < G, a, q);
+    const int n = min(rec.x + 1, L.C), nb = (n + BT - 1) / BT;
+    const int tail = rec.z / BT;  // the block that the new token goes to
+    float* xs = FUSED ? s_x : L.logits + (size_t)u * G * L.cpad;
     Softmax<D> s;
     s.clear();
 
-    auto load = [&](int b, u32x4 (&kr)[NP], u32x4 (&vr)[NP]) {
-        const size_t at = (size_t)min(b, nb - 1) * BT * D + lane * VE;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) kr[i] = ld16(Ku + at + i * 64 * VE);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) vr[i] = ld16(Vu + at + i * 64 * VE);
-    };
     auto block = [&](int b, u32x4 (&kr)[NP], u32x4 (&vr)[NP]) {
         if (b == tail) {
             const int t = rec.z - b * BT, e = t % VE;
@@ -346,23 +449,22 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         attend<T, D>(kr, vr, q, valid, a, L.scale_log2, s, x);
         if (col < G)
 #pragma unroll
-            for (int t = 0; t < QT; ++t)
-                *reinterpret_cast<f32x4*>(xs + (size_t)col * L.cpad + b * BT + VE * a + 4 * t) = x[t];
+            for (int t = 0; t < QT; ++t) {
+                float* to = xs + (size_t)col * L.cpad + b * BT + VE * a + 4 * t;
+                if constexpr (FUSED) *reinterpret_cast<f32x4*>(to) = x[t];
+                else publish4(to, x[t]);
+            }
     };
-
-    if (lo + w < hi) {
-        u32x4 k0[NP], v0[NP], k1[NP], v1[NP];
-        int b = lo + w;
-        load(b, k0, v0);
+    if (b < nb) {
         while (true) {
-            load(b + NW, k1, v1);
+            load(b + step, k1, v1);
             block(b, k0, v0);
-            b += NW;
-            if (b >= hi) break;
-            load(b + NW, k0, v0);
+            b += step;
+            if (b >= nb) break;
+            load(b + step, k0, v0);
             block(b, k1, v1);
-            b += NW;
-            if (b >= hi) break;
+            b += step;
+            if (b >= nb) break;
         }
     }
     s.l = sum_groups(s.l);
@@ -379,9 +481,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     auto ml = [&](int i, int g) { return make_float2(s_ml[2 * (i * 16 + g)], s_ml[2 * (i * 16 + g) + 1]); };
     auto o = [&](int i, int g, int c) { return s_o[(size_t)(i * G + g) * (D + 4) + c]; };
     if constexpr (FUSED) {
-        finish_step<T, D, NW * 64>(L, io, u, rec, s_x, L.cpad, NW, ml, o);
+        auto x4 = [&](int g, int j) { return *reinterpret_cast<const f32x4*>(s_x + (size_t)g * L.cpad + j); };
+        finish_step<T, D, NW>(L, io, u, rec, NW, s_w, ml, o, x4);
     } else {
-        const size_t part = (size_t)u * L.nsplit + split;
+        float* mlp = L.ml + (size_t)u * nsplit * G * 2;
+        float* part = L.part + (size_t)u * nsplit * G * D;
         for (int i = tid; i < G * D; i += NW * 64) {
             const int g = i / D, c = i % D;
             float M = -INFINITY, x = 0.0f, z = 0.0f;
@@ -394,49 +498,46 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 x += o(k, g, c) * e;
                 z += ml(k, g).y * e;
             }
-            L.part[(part * G + g) * D + c] = x;
+            publish(part + (size_t)(split * G + g) * D + c, x);
             if (c == 0) {
-                L.ml[2 * (part * G + g)] = M;
-                L.ml[2 * (part * G + g) + 1] = z;
+                publish(mlp + 2 * (split * G + g), M);
+                publish(mlp + 2 * (split * G + g) + 1, z);
             }
         }
+        if (!arrive_last(L.arrived + u, nsplit)) return;
+        auto gml = [&](int i, int g) {
+            return make_float2(published(mlp + 2 * (i * G + g)), published(mlp + 2 * (i * G + g) + 1));
+        };
+        auto go = [&](int i, int g, int c) { return published(part + (size_t)(i * G + g) * D + c); };
+        auto x4 = [&](int g, int j) { return published4(xs + (size_t)g * L.cpad + j); };
+        finish_step<T, D, NW>(L, io, u, rec, nsplit, s_w, gml, go, x4);
     }
 }
 
-// The end of a step whose units are split: one workgroup per unit.
-constexpr int kFinishThreads = 1024;
-template <typename T, int D>
-__global__ __launch_bounds__(kFinishThreads) void k_weight_finish(WeightView L, WeightStepIO io) {
-    const int u = blockIdx.x, G = L.G;
-    if (io.active != nullptr && io.active[u / L.nkv] == 0) return;
-    const int4 rec = *reinterpret_cast<const int4*>(L.unit + (size_t)u * kWeightFields);
-    const float* mlp = L.ml + (size_t)u * L.nsplit * G * 2;
-    const float* part = L.part + (size_t)u * L.nsplit * G * D;
-    auto ml = [&](int i, int g) { return make_float2(mlp[2 * (i * G + g)], mlp[2 * (i * G + g) + 1]); };
-    auto o = [&](int i, int g, int c) { return part[(size_t)(i * G + g) * D + c]; };
-    finish_step<T, D, kFinishThreads>(L, io, u, rec, L.logits + (size_t)u * G * L.cpad, L.cpad, L.nsplit, ml, o);
+// Floats of the parts' shares: those of the workgroup's wavefronts or splits, and of the prefix.
+int share_floats(int G, int parts) { return (G * parts + 3) / 4 * 4; }
+
+size_t step_lds(int G, int D, int cpad, int nw, bool fused, int parts) {
+    return sizeof(float) * ((size_t)nw * 32 + share_floats(G, parts) + (size_t)nw * G * (D + 4) +
+                            (fused ? (size_t)G * cpad : 0));
 }
 
-size_t step_lds(int G, int D, int cpad, int nw, bool fused) {
-    return sizeof(float) * ((size_t)nw * 32 + (size_t)nw * G * (D + 4) + (fused ? (size_t)G * cpad : 0));
+template <typename T, int D, int NW>
+hipError_t launch_step_t(const WeightView& L, const WeightStepIO& io, const WeightPlan& p, size_t lds, hipStream_t s) {
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)L.U * p.nsplit), dim3(NW * 64), lds, s, L, io);
+        return hipGetLastError();
+    };
+    if (p.stream) return p.fused ? go(k_weight_step<T, D, NW, true, true>) : go(k_weight_step<T, D, NW, false, true>);
+    return p.fused ? go(k_weight_step<T, D, NW, true, false>) : go(k_weight_step<T, D, NW, false, false>);
 }
 
-template <typename T, int D>
-hipError_t launch_step_t(const WeightView& L, const WeightStepIO& io, const WeightPlan& p, hipStream_t s) {
-    const dim3 grid((unsigned)L.U * p.nsplit), wg(p.waves * 64);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, p.lds, s, L, io); };
-    if (p.waves == 8) p.fused ? go(k_weight_step<T, D, 8, true>) : go(k_weight_step<T, D, 8, false>);
-    else p.fused ? go(k_weight_step<T, D, 4, true>) : go(k_weight_step<T, D, 4, false>);
-    if (!p.fused)
-        hipLaunchKernelGGL((k_weight_finish<T, D>), dim3(L.U), dim3(kFinishThreads), 0, s, L, io);
-    return hipGetLastError();
-}
-
-template <typename T, int D>
+template <typename T, int D, int NW>
 hipError_t allow_t() {
     hipError_t e = hipSuccess;
-    for (const void* f : {(const void*)k_weight_step<T, D, 8, true>, (const void*)k_weight_step<T, D, 8, false>,
-                          (const void*)k_weight_step<T, D, 4, true>, (const void*)k_weight_step<T, D, 4, false>}) {
+    for (const void* f : {(const void*)k_weight_step<T, D, NW, true, false>, (const void*)k_weight_step<T, D, NW, true, true>,
+                          (const void*)k_weight_step<T, D, NW, false, false>,
+                          (const void*)k_weight_step<T, D, NW, false, true>}) {
         const hipError_t r = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kStepLds);
         if (r != hipSuccess) e = r;
     }
@@ -461,21 +562,29 @@ void launch_store(int D, bool bf16, void* K, void* V, const void* k, const void*
 
 }  // namespace
 
-WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16) {
+WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16, double layer_bytes) {
     const int bt = bf16 ? 32 : 16, nb = (C + bt - 1) / bt, cpad = nb * bt;
     WeightPlan p{};
+    auto fits = [&](int nw, int per_cu) {
+        return per_cu * (step_lds(G, D, cpad, nw, true, nw + kMaxPrefixParts) + 1024) <= kStepLds;
+    };
     p.waves = 8;
-    if (step_lds(G, D, cpad, 8, false) > kStepLds / 2) p.waves = 4;
-    const int want = std::min(std::max(512 / U, 1), std::max(1, nb / p.waves));
-    p.fused = want == 1 && step_lds(G, D, cpad, p.waves, true) <= kStepLds;
-    p.nsplit = p.fused ? 1 : std::max(want, 1);
-    p.lds = step_lds(G, D, cpad, p.waves, p.fused);
+    if (U > 256 && fits(4, 2)) p.waves = 4;
+    if (step_lds(G, D, cpad, 8, false, kMaxStepSplits + kMaxPrefixParts) > kStepLds) p.waves = 4;
+    const int want = U >= 192 || nb <= 32 ? 1 : std::min({512 / U, (nb + p.waves - 1) / p.waves, kMaxStepSplits});
+    p.fused = want <= 1 && fits(p.waves, 1);
+    p.nsplit = std::max(want, 1);
+    p.stream = layer_bytes > 300e6;
     return p;
 }
 
-hipError_t weight_allow_lds(bool bf16, int D) {
-    if (bf16) return D == 128 ? allow_t<uint16_t, 128>() : allow_t<uint16_t, 64>();
-    return D == 128 ? allow_t<float, 128>() : allow_t<float, 64>();
+hipError_t weight_allow_lds(bool bf16, int D, int waves) {
+    auto go = [&](auto w) {
+        constexpr int NW = decltype(w)::value;
+        if (bf16) return D == 128 ? allow_t<uint16_t, 128, NW>() : allow_t<uint16_t, 64, NW>();
+        return D == 128 ? allow_t<float, 128, NW>() : allow_t<float, 64, NW>();
+    };
+    return waves == 8 ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 4>{});
 }
 
 hipError_t launch_weight_prefill(const WeightView& L, bool bf16, const void* k, const void* v, const float* weights,
@@ -489,10 +598,20 @@ hipError_t launch_weight_prefill(const WeightView& L, bool bf16, const void* k, 
     return hipGetLastError();
 }
 
-hipError_t launch_weight_step(const WeightView& L, bool bf16, const WeightStepIO& io, const WeightPlan& p,
+hipError_t launch_weight_step(const WeightView& view, bool bf16, const WeightStepIO& io, const WeightPlan& p,
                               hipStream_t s) {
-    if (bf16) return L.D == 128 ? launch_step_t<uint16_t, 128>(L, io, p, s) : launch_step_t<uint16_t, 64>(L, io, p, s);
-    return L.D == 128 ? launch_step_t<float, 128>(L, io, p, s) : launch_step_t<float, 64>(L, io, p, s);
+    WeightView L = view;
+    const int parts = (p.fused ? p.waves : p.nsplit) + io.prefix.n;
+    L.wfloats = share_floats(L.G, parts);
+    const size_t lds = step_lds(L.G, L.D, L.cpad, p.waves, p.fused, parts);
+    auto go = [&](auto w) {
+        constexpr int NW = decltype(w)::value;
+        if (bf16)
+            return L.D == 128 ? launch_step_t<uint16_t, 128, NW>(L, io, p, lds, s)
+                              : launch_step_t<uint16_t, 64, NW>(L, io, p, lds, s);
+        return L.D == 128 ? launch_step_t<float, 128, NW>(L, io, p, lds, s) : launch_step_t<float, 64, NW>(L, io, p, lds, s);
+    };
+    return p.waves == 8 ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 4>{});
 }
 
 hipError_t launch_prefix_store(void* K, void* V, int32_t* len, int nkv, int D, int tpad, bool bf16, const void* k,

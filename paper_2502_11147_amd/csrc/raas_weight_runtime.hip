@@ -99,7 +99,7 @@ struct raas_weight_cache {
     bool bf16;
     WeightPlan plan;
     void *K = nullptr, *V = nullptr;
-    int32_t *pos = nullptr, *unit = nullptr;
+    int32_t *pos = nullptr, *unit = nullptr, *arrived = nullptr;
     float *w = nullptr, *logits = nullptr, *part = nullptr, *ml = nullptr;
     size_t bytes = 0;
     std::vector<unsigned char> prefilled;
@@ -125,12 +125,13 @@ WeightView view(const raas_weight_cache* c, int layer) {
     const size_t kv = (size_t)layer * c->U * c->cpad * c->cfg.head_dim * (c->bf16 ? 2 : 4);
     L.K = (char*)c->K + kv;
     L.V = (char*)c->V + kv;
-    L.pos = c->pos + (size_t)layer * c->U * c->C;
-    L.w = c->w + (size_t)layer * c->U * c->C;
+    L.pos = c->pos + (size_t)layer * c->U * c->cpad;
+    L.w = c->w + (size_t)layer * c->U * c->cpad;
     L.unit = c->unit + (size_t)layer * c->U * kWeightFields;
     L.logits = c->logits;
     L.part = c->part;
     L.ml = c->ml;
+    L.arrived = c->arrived;
     L.U = c->U;
     L.G = c->G;
     L.D = c->cfg.head_dim;
@@ -179,6 +180,23 @@ raas_status prefix_parts(raas_prefix* p, int32_t layer, const void* q, int rows,
     return RAAS_OK;
 }
 
+// A launch of the prompt weights: its sequences, its plan, the floats of its scratch.
+struct PromptSpace {
+    int nseq;
+    PromptPlan plan;
+    size_t lse, ml, part;
+};
+PromptSpace prompt_space(int batch, int n_q_heads, int n_kv_heads, int max_len, int window, bool bf16) {
+    PromptSpace sp;
+    sp.nseq = std::min({batch, kLenSeqs, std::max(1, 65535 / n_kv_heads)});
+    const int W = std::min(window, max_len);
+    sp.plan = plan_prompt(sp.nseq * n_kv_heads, n_q_heads / n_kv_heads, W, max_len, bf16);
+    sp.lse = (size_t)sp.nseq * n_q_heads * W;
+    sp.ml = sp.plan.chunks > 1 ? sp.lse * sp.plan.chunks * 2 : 0;
+    sp.part = sp.plan.row_chunks > 1 ? (size_t)sp.plan.row_chunks * sp.nseq * n_kv_heads * max_len : 0;
+    return sp;
+}
+
 }  // namespace
 
 extern "C" {
@@ -205,25 +223,26 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
         c->G = cfg->n_q_heads / cfg->n_kv_heads;
         c->C = cfg->capacity;
         c->cpad = pad_tokens(cfg->capacity, c->bf16);
+        const size_t Ly = (size_t)cfg->n_layers, U = (size_t)c->U, d = (size_t)cfg->head_dim, esz = c->bf16 ? 2 : 4;
+        c->plan = plan_weight_step(c->U, c->G, cfg->head_dim, c->C, c->bf16, 2.0 * Ly * U * c->cpad * d * esz);
         hipError_t e = hipGetDevice(&c->device);
-        if (e == hipSuccess) e = weight_allow_lds(c->bf16, cfg->head_dim);
+        if (e == hipSuccess) e = weight_allow_lds(c->bf16, cfg->head_dim, c->plan.waves);
         if (e != hipSuccess) {
             delete c;
             return hip_fail(e, "hipFuncSetAttribute");
         }
-        c->plan = plan_weight_step(c->U, c->G, cfg->head_dim, c->C, c->bf16);
-        const size_t Ly = (size_t)cfg->n_layers, U = (size_t)c->U, d = (size_t)cfg->head_dim, esz = c->bf16 ? 2 : 4;
         const bool split = !c->plan.fused;
         const size_t parts = split ? U * c->plan.nsplit * c->G : 1;
         const std::vector<Req> reqs = {
             {&c->K, Ly * U * c->cpad * d * esz},
             {&c->V, Ly * U * c->cpad * d * esz},
-            {(void**)&c->pos, Ly * U * c->C * 4},
-            {(void**)&c->w, Ly * U * c->C * 4},
+            {(void**)&c->pos, Ly * U * c->cpad * 4},
+            {(void**)&c->w, Ly * U * c->cpad * 4},
             {(void**)&c->unit, Ly * U * kWeightFields * 4},
             {(void**)&c->logits, split ? U * c->G * c->cpad * 4 : 4},
             {(void**)&c->part, parts * d * 4},
             {(void**)&c->ml, parts * 2 * 4},
+            {(void**)&c->arrived, U * 4},
         };
         const raas_status sa = allocate(reqs, c->bytes, (hipStream_t)stream);
         if (sa != RAAS_OK) {
@@ -244,7 +263,7 @@ void raas_destroy_weight_cache(raas_weight_cache* c) {
     DeviceScope scope(c->device);
     if (c->K) (void)hipStreamSynchronize(c->last_stream);
     for (void* p : {c->K, c->V, (void*)c->pos, (void*)c->w, (void*)c->unit, (void*)c->logits, (void*)c->part,
-                    (void*)c->ml})
+                    (void*)c->ml, (void*)c->arrived})
         if (p) (void)hipFree(p);
     delete c;
 }
@@ -331,15 +350,16 @@ raas_status raas_weight_export_state(raas_weight_cache* c, int32_t layer, int32_
     if (scope.error() != hipSuccess) return hip_fail(scope.error(), "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
     const WeightView L = view(c, layer);
-    const size_t n = (size_t)c->U * c->C;
+    const size_t row = (size_t)c->C * 4, pitch = (size_t)c->cpad * 4;
     std::vector<int32_t> unit;
     try {
         unit.resize((size_t)c->U * kWeightFields);
     } catch (const std::bad_alloc&) {
         return fail(RAAS_E_OOM, "host allocation failed");
     }
-    hipError_t e = hipMemcpyAsync(positions, L.pos, n * 4, hipMemcpyDeviceToHost, s);
-    if (e == hipSuccess) e = hipMemcpyAsync(weights, L.w, n * 4, hipMemcpyDeviceToHost, s);
+    hipError_t e = hipMemcpy2DAsync(positions, row, L.pos, pitch, row, (size_t)c->U, hipMemcpyDeviceToHost, s);
+    if (e == hipSuccess)
+        e = hipMemcpy2DAsync(weights, row, L.w, pitch, row, (size_t)c->U, hipMemcpyDeviceToHost, s);
     if (e == hipSuccess) e = hipMemcpyAsync(unit.data(), L.unit, unit.size() * 4, hipMemcpyDeviceToHost, s);
     if (e != hipSuccess) return hip_fail(e, "hipMemcpyAsync");
     e = hipStreamSynchronize(s);
@@ -456,9 +476,12 @@ size_t raas_prompt_weights_workspace(int32_t batch, int32_t n_q_heads, int32_t n
     if (batch < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || max_len < 1 ||
         window < 1)
         return 0;
-    const int nseq = std::min({batch, kLenSeqs, std::max(1, 65535 / n_kv_heads)});
-    const int W = std::min(window, max_len), G = n_q_heads / n_kv_heads;
-    return (size_t)nseq * n_q_heads * W * plan_prompt_chunks(nseq * n_kv_heads, G, W, max_len) * 2 * sizeof(float);
+    size_t most = 0;  // over both types, which are cut differently
+    for (bool bf16 : {false, true}) {
+        const PromptSpace sp = prompt_space(batch, n_q_heads, n_kv_heads, max_len, window, bf16);
+        most = std::max(most, sp.lse + sp.ml + sp.part);
+    }
+    return most * sizeof(float);
 }
 
 raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
@@ -480,13 +503,16 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
     const size_t need = raas_prompt_weights_workspace(batch, n_q_heads, n_kv_heads, max_len, window);
     if (!workspace || workspace_bytes < need)
         return fail(RAAS_E_INVALID, "workspace must hold %zu bytes (got %zu)", need, workspace ? workspace_bytes : 0);
-    const int most = std::min({batch, kLenSeqs, std::max(1, 65535 / n_kv_heads)});
+    const PromptSpace sp = prompt_space(batch, n_q_heads, n_kv_heads, max_len, window, dtype == RAAS_BF16);
     PromptView v{};
+    static_cast<PromptPlan&>(v) = sp.plan;
     v.q = q;
     v.k = k;
     v.prefix_lse = prefix_lse;
     v.weights = weights;
-    v.ml = (float*)workspace;
+    v.lse = (float*)workspace;
+    v.ml = v.lse + sp.lse;
+    v.part = v.ml + sp.ml;
     v.W = window;
     v.P = max_len;
     v.G = n_q_heads / n_kv_heads;
@@ -494,12 +520,10 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
     v.nkv = n_kv_heads;
     v.g_magic = v.G > 1 ? (uint32_t)(((1ull << 32) + v.G - 1) / v.G) : 0;
     v.scale_log2 = scale_log2(head_dim);
-    v.chunks = plan_prompt_chunks(most * n_kv_heads, v.G, window, max_len);
-    v.chunk_keys = ((max_len + v.chunks - 1) / v.chunks + 63) / 64 * 64;
-    for (int b = 0; b < batch; b += most) {
+    for (int b = 0; b < batch; b += sp.nseq) {
         SeqLens sl{};
         v.seq0 = b;
-        v.nseq = std::min(most, batch - b);
+        v.nseq = std::min(sp.nseq, batch - b);
         fill_lens(sl, lens, nullptr, max_len, b, v.nseq);
         const hipError_t e = launch_prompt_weights(v, dtype == RAAS_BF16, sl, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, "prompt weights launch");
