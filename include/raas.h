@@ -316,7 +316,7 @@ typedef struct raas_weight_cache raas_weight_cache; /* opaque */
 typedef struct {
     int32_t n_layers, n_q_heads, n_kv_heads, head_dim; /* as above */
     int32_t max_tokens; /* tokens that a layer may store, 1 .. 1048576 */
-    int32_t max_rows;   /* sequences per call, >= 1; max_rows * n_q_heads <= 16777216 */
+    int32_t max_rows;   /* sequences per call, >= 1; max_rows * n_q_heads <= 131072 */
     int32_t dtype;      /* raas_dtype */
 } raas_prefix_config;
 

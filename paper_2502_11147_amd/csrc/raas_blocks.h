@@ -34,6 +34,15 @@ constexpr int kTokens = 4 * kVec<T>;  // tokens of a block
 template <typename T>
 constexpr int kTiles = kVec<T> / 4;  // 16-token tiles of a block
 
+// Workgroup barrier that waits for this wavefront's LDS traffic only: loads
+// already issued to global memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0); vmcnt and expcnt left at their maxima
+    __builtin_amdgcn_s_barrier();
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
+
 // This wavefront's number in its workgroup, as a scalar.
 __device__ __forceinline__ int wave_of(int tid) { return __builtin_amdgcn_readfirstlane(tid >> 6); }
 
@@ -124,6 +133,25 @@ __device__ __forceinline__ void load_row(const T* row, bool real, int a, u32x4 (
         q[ks] = real ? ld16_in<T>(row + 4 * kVec<T> * ks + kVec<T> * a) : u32x4{0u, 0u, 0u, 0u};
 }
 
+// VE probabilities as the operand that multiplies values: rounded to bf16 beside
+// bf16 values (the matrix cores take no other type there; the errors, half a step
+// of 2^-8 each, average out over the tokens and stay below the output's own
+// rounding).
+template <typename T>
+__device__ __forceinline__ u32x4 pack(const float (&p)[kVec<T>]) {
+    u32x4 v;
+    if constexpr (sizeof(T) == 2) {
+        bf16x8 b;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = (__bf16)p[j];
+        v = __builtin_bit_cast(u32x4, b);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(p[j]);
+    }
+    return v;
+}
+
 // Running softmax of one query column: maximum (base 2), this lane's share of
 // the sum, and the accumulated values' rows 16 ct + 4 a + r.
 template <int D>
@@ -180,16 +208,7 @@ __device__ __forceinline__ void attend(const u32x4 (&kr)[D / 16], const u32x4 (&
             p[4 * t + r] = __builtin_amdgcn_exp2f(x[t][r] - s.m);
             s.l += p[4 * t + r];
         }
-    u32x4 pv;
-    if constexpr (sizeof(T) == 2) {
-        bf16x8 b;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = (__bf16)p[j];
-        pv = __builtin_bit_cast(u32x4, b);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) pv[j] = __float_as_uint(p[j]);
-    }
+    const u32x4 pv = pack<T>(p);
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct) s.o[ct] = mfma16<T>(vr[ct], pv, s.o[ct]);
 }

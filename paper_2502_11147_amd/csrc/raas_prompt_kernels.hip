@@ -144,9 +144,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     Staged<T, D> next;
     next.load(tid, [&](int r) { return K + (size_t)min(lo + r, len - 1) * D; });
     for (int j0 = lo; j0 < hi; j0 += kStage) {
-        __syncthreads();
+        lds_barrier();
         next.store(tid, s_k);
-        __syncthreads();
+        lds_barrier();
         if (j0 + kStage < hi) next.load(tid, [&](int r) { return K + (size_t)min(j0 + kStage + r, len - 1) * D; });
         if (j0 >= mine) continue;
         const int jw = j0 + (ROWS ? 0 : w * 16 * SUB);
@@ -259,10 +259,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const int start = max(lo, first) / kStage * kStage;
     if (start < hi) load(start);
     for (int r0 = start; r0 < hi; r0 += kStage) {
-        __syncthreads();
+        lds_barrier();
         next.store(tid, s_q);
         if (tid < kStage) s_lse[tid] = lse;
-        __syncthreads();
+        lds_barrier();
         if (r0 + kStage < hi) load(r0 + kStage);
         if (r0 + kStage <= mine || j0 >= len) continue;
         // (two bodies: a branch inside would keep products and exponentials apart)

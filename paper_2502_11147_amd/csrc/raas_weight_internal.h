@@ -88,13 +88,11 @@ struct PrefixView {
     int nsplit;
     float scale_log2;
 };
-struct PrefixPlan {
-    int nsplit;
-};
-PrefixPlan plan_prefix(int nkv, int rows, int D, int tokens, bool bf16);
+// Parts that the attention of `rows` rows per KV head is cut into.
+int plan_prefix(int nkv, int rows, int tokens, bool bf16);
 // Rows of the parts that attention of up to `rows` rows may write, whatever is
 // stored: sizes the scratch.
-size_t prefix_scratch_rows(int nkv, int rows, int D, bool bf16);
+size_t prefix_scratch_rows(int nkv, int rows);
 hipError_t launch_prefix_store(void* K, void* V, int32_t* len, int nkv, int D, int tpad, bool bf16, const void* k,
                                const void* v, int tokens, hipStream_t s);
 hipError_t launch_prefix_attention(const PrefixView& P, bool bf16, const void* q, hipStream_t s);

@@ -18,6 +18,8 @@ namespace {
 
 // Tokens that a unit of a cache, a prefix or a prompt may have.
 constexpr int kMaxTokens = 1 << 20;
+// Query rows of one call over a prefix (the grids' limit).
+constexpr int kMaxQueries = 1 << 17;
 
 // The handle's device for the length of a call.
 class DeviceScope {
@@ -172,7 +174,7 @@ raas_status prefix_parts(raas_prefix* p, int32_t layer, const void* q, int rows,
     P.D = p->cfg.head_dim;
     P.tpad = p->tpad;
     P.rows = rows * p->G;
-    P.nsplit = plan_prefix(P.nkv, P.rows, P.D, p->stored[layer], p->bf16).nsplit;
+    P.nsplit = plan_prefix(P.nkv, P.rows, p->stored[layer], p->bf16);
     P.scale_log2 = scale_log2(P.D);
     const hipError_t e = launch_prefix_attention(P, p->bf16, q, s);
     if (e != hipSuccess) return hip_fail(e, "prefix attention launch");
@@ -383,8 +385,8 @@ raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas
     if (st != RAAS_OK) return st;
     if (cfg->max_tokens < 1 || cfg->max_tokens > kMaxTokens)
         return fail(RAAS_E_INVALID, "max_tokens must lie in [1, %d] (got %d)", kMaxTokens, cfg->max_tokens);
-    if (cfg->max_rows < 1 || (double)cfg->max_rows * cfg->n_q_heads > 1 << 24)
-        return fail(RAAS_E_INVALID, "max_rows must be >= 1, and max_rows * n_q_heads at most %d (got %d rows)", 1 << 24,
+    if (cfg->max_rows < 1 || (double)cfg->max_rows * cfg->n_q_heads > kMaxQueries)
+        return fail(RAAS_E_INVALID, "max_rows must be >= 1, and max_rows * n_q_heads at most %d (got %d rows)", kMaxQueries,
                     cfg->max_rows);
     raas_prefix* p = nullptr;
     try {
@@ -400,7 +402,7 @@ raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas
             return hip_fail(e, "hipGetDevice");
         }
         const size_t Ly = (size_t)cfg->n_layers, d = (size_t)cfg->head_dim, esz = p->bf16 ? 2 : 4;
-        const size_t parts = prefix_scratch_rows(cfg->n_kv_heads, cfg->max_rows * p->G, cfg->head_dim, p->bf16);
+        const size_t parts = prefix_scratch_rows(cfg->n_kv_heads, cfg->max_rows * p->G);
         const std::vector<Req> reqs = {
             {&p->K, Ly * cfg->n_kv_heads * p->tpad * d * esz},
             {&p->V, Ly * cfg->n_kv_heads * p->tpad * d * esz},

@@ -26,22 +26,24 @@ def _dtype_code(dtype: str) -> int:
 
 
 def _pointer(t, name, dtype, shape, device, optional=False):
-    """Address of a contiguous device tensor of this type, shape and device."""
+    """Address of a contiguous device tensor of this type, shape and device index."""
     if t is None and optional:
         return None
-    torch = _torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    try:
+        if t.get_device() == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA (HIP) tensor" % name)
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device.index != device:
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d (got %s %s on %s)"
-                         % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
-    return ctypes.c_void_p(t.data_ptr())
+    raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d (got %s %s on %s)"
+                     % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
 
 def _stream(stream, device):
     if stream is None:
         stream = _torch().cuda.current_stream(device)
-    return ctypes.c_void_p(stream.cuda_stream)
+    return stream.cuda_stream
 
 
 def _host_ints(values, n, name):
@@ -64,6 +66,7 @@ class _Handle:
         self.lib = load_library()
         self.cfg, self.dtype = config, dtype
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self._float32, self._int32 = torch.float32, torch.int32
         self.device = torch.cuda.current_device()
         self._h = ctypes.c_void_p()
         _check(getattr(self.lib, create)(ctypes.byref(config), _stream(stream, self.device), ctypes.byref(self._h)),
@@ -88,8 +91,11 @@ class _Handle:
     def _tensor(self, t, shape, name, optional=False):
         return _pointer(t, name, self.torch_dtype, shape, self.device, optional)
 
-    def _typed(self, t, dtype, shape, name):
-        return _pointer(t, name, getattr(_torch(), dtype), shape, self.device, optional=True)
+    def _floats(self, t, shape, name):
+        return _pointer(t, name, self._float32, shape, self.device, optional=True)
+
+    def _ints(self, t, shape, name):
+        return _pointer(t, name, self._int32, shape, self.device, optional=True)
 
 
 class SharedPrefix(_Handle):
@@ -117,10 +123,10 @@ class SharedPrefix(_Handle):
         """Attention of q [rows][n_q_heads][head_dim] over the layer's prefix
         into out (same shape) and lse (fp32 [rows][n_q_heads], optional)
         (raas_prefix_attention)."""
-        rows = int(q.shape[0])
+        rows = q.shape[0]
         shape = (rows, self.n_q_heads, self.head_dim)
         qp, op = self._tensor(q, shape, "q"), self._tensor(out, shape, "out")
-        lp = self._typed(lse, "float32", shape[:2], "lse")
+        lp = self._floats(lse, shape[:2], "lse")
         _check(self.lib.raas_prefix_attention(self._h, layer, qp, rows, op, lp, _stream(stream, self.device)),
                "raas_prefix_attention")
 
@@ -159,7 +165,7 @@ class WeightCache(_Handle):
         shape = (B, self.n_kv_heads, max_len, self.head_dim)
         kp = self._tensor(k, shape, "k") if max_len else None
         vp = self._tensor(v, shape, "v") if max_len else None
-        wp = self._typed(weights, "float32", shape[:3], "weights") if max_len else None
+        wp = self._floats(weights, shape[:3], "weights") if max_len else None
         _check(self.lib.raas_weight_prefill(self._h, layer, kp, vp, wp, _host_ints(lens, B, "lens"),
                                             _host_ints(None if mask is None else [bool(x) for x in mask], B, "mask"),
                                             max_len, _stream(stream, self.device)), "raas_weight_prefill")
@@ -180,10 +186,10 @@ class WeightCache(_Handle):
             self._tensor(k_new, (B, Hkv, d), "k_new"),
             self._tensor(v_new, (B, Hkv, d), "v_new"),
             self._tensor(out, (B, Hq, d), "out"),
-            self._typed(positions, "int32", (B, Hkv, C), "positions"),
-            self._typed(weights, "float32", (B, Hkv, C), "weights"),
-            self._typed(evicted, "int32", (B, Hkv), "evicted"),
-            self._typed(active, "int32", (B,), "active"),
+            self._ints(positions, (B, Hkv, C), "positions"),
+            self._floats(weights, (B, Hkv, C), "weights"),
+            self._ints(evicted, (B, Hkv), "evicted"),
+            self._ints(active, (B,), "active"),
             None if prefix is None else prefix.handle,
             _stream(stream, self.device),
         ))
@@ -246,5 +252,5 @@ def prompt_weights(q, k, weights, lens=None, prefix_lse=None, stream=None):
     with torch.cuda.device(dev), torch.cuda.stream(stream):
         space = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
         _check(lib.raas_prompt_weights(B, Hq, Hkv, d, code, qp, kp, lp, _host_ints(lens, B, "lens"), P, W, wp,
-                                       ctypes.c_void_p(space.data_ptr()), need, ctypes.c_void_p(stream.cuda_stream)),
+                                       space.data_ptr(), need, stream.cuda_stream),
                "raas_prompt_weights")
