@@ -111,6 +111,51 @@ __device__ __forceinline__ float sum_groups(float x) {
     return __builtin_bit_cast(float, (unsigned)b[0]) + __builtin_bit_cast(float, (unsigned)b[1]);
 }
 
+// Moves within 16 lanes that stay in the vector unit: 0xB1 and 0x4E swap
+// neighbours and pairs, 0x141 and 0x140 mirror eight and sixteen lanes (whose
+// halves hold equal values by then).
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float x) { return __uint_as_float(dpp<CTRL>(__float_as_uint(x))); }
+// max and sum over a wavefront, the same on each lane
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, dpp_f<0xB1>(x));
+    x = fmaxf(x, dpp_f<0x4E>(x));
+    x = fmaxf(x, dpp_f<0x141>(x));
+    x = fmaxf(x, dpp_f<0x140>(x));
+    return max_groups(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += dpp_f<0xB1>(x);
+    x += dpp_f<0x4E>(x);
+    x += dpp_f<0x141>(x);
+    x += dpp_f<0x140>(x);
+    return sum_groups(x);
+}
+// min of 64-bit values over a wavefront, the same on each lane
+__device__ __forceinline__ unsigned long long wave_min(unsigned long long x) {
+    auto with = [&](uint32_t lo, uint32_t hi) {
+        const unsigned long long y = (unsigned long long)hi << 32 | lo;
+        x = y < x ? y : x;
+    };
+    with(dpp<0xB1>((uint32_t)x), dpp<0xB1>((uint32_t)(x >> 32)));
+    with(dpp<0x4E>((uint32_t)x), dpp<0x4E>((uint32_t)(x >> 32)));
+    with(dpp<0x141>((uint32_t)x), dpp<0x141>((uint32_t)(x >> 32)));
+    with(dpp<0x140>((uint32_t)x), dpp<0x140>((uint32_t)(x >> 32)));
+    auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(x >> 32), (uint32_t)(x >> 32), false, false);
+    with(lo[0], hi[0]);
+    with(lo[1], hi[1]);
+    lo = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+    hi = __builtin_amdgcn_permlane32_swap((uint32_t)(x >> 32), (uint32_t)(x >> 32), false, false);
+    with(lo[0], hi[0]);
+    with(lo[1], hi[1]);
+    return x;
+}
+
 // c += A B for one 16-byte vector of either operand per lane: 4 VE channels.
 template <typename T>
 __device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, f32x4 c) {

@@ -21,7 +21,8 @@ namespace {
 using namespace blk;
 
 constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
+constexpr int kThreads = 256;  // of the kernels that join and add
+constexpr float kNothing = -1e30f;  // the maximum (base 2) of no logits: finite, so that no difference is NaN
 constexpr int kStage = 64;  // rows (keys of the first kernel, queries of the second) that a workgroup stages in LDS
 // 16-row tiles that a wavefront holds in registers
 template <typename T>
@@ -43,20 +44,25 @@ __device__ __forceinline__ const T* query_row(const PromptView& v, int b, int h,
 // read fall on different banks.
 template <typename T, int D>
 struct Staged {
-    static constexpr int NCH = D / kVec<T>, PER = kStage * NCH / kThreads;  // pieces of a row, and of a thread
+    static constexpr int HALVES = D * sizeof(T) > 256 ? 1 : 2;  // of LDS, filled in turn: 32 KB in all either way
+    static constexpr int NT = kWaves * 64, NCH = D / kVec<T>, PER = kStage * NCH / NT;  // pieces of a row, and of a thread
     u32x4 x[PER];
     template <class Row>
     __device__ __forceinline__ void load(int tid, Row row) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int p = tid + i * kThreads;
+            const int p = tid + i * NT;
             x[i] = ld16_in<T>(row(p / NCH) + (p % NCH) * kVec<T>);
         }
     }
+    // Puts the rows into LDS, where every wavefront may read them afterwards.
+    // (With two halves all have read what this one held before: their reads of it
+    // came before the last barrier.)
     __device__ __forceinline__ void store(int tid, u32x4* s) const {
+        if constexpr (HALVES == 1) lds_barrier();
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int p = tid + i * kThreads, r = p / NCH;
+            const int p = tid + i * NT, r = p / NCH;
             s[r * NCH + ((p % NCH) ^ (r & (NCH - 1)))] = x[i];
         }
     }
@@ -109,47 +115,46 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(PromptView v, SeqLens 
 // Maximum (base 2) and sum of every query row over a chunk of keys. Grid:
 // units, row tiles (the ones that see the most keys first), key chunks: the
 // workgroups that follow each other have equal work, and with eight units each
-// XCD's L2 serves one. ROWS: the
-// wavefronts take RT tiles of 16 rows each and share the staged keys; else (few
-// rows) all take the same RT tiles, and a quarter of the staged keys each.
-template <typename T, int D, int RT, bool ROWS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_rows(PromptView v, SeqLens lens) {
-    constexpr int KS = D / (4 * kVec<T>), SUB = ROWS ? kStage / 16 : kStage / 16 / kWaves;
-    __shared__ __align__(16) u32x4 s_k[kStage * D / kVec<T>];
-    __shared__ float s_m[ROWS ? 1 : kWaves][RT * 16], s_l[ROWS ? 1 : kWaves][RT * 16];
+// XCD's L2 serves one (row tiles first, some shader engines always got the long
+// ones: 125 us for 100). KW wavefronts share RT tiles of 16 rows and take a part
+// of the staged keys each. LDS bounds it besides the exponentials (it gives a CU
+// some 60 bytes a cycle): the more rows a wavefront holds, the fewer of its
+// reads a product takes.
+template <typename T, int D, int RT, int KW>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_rows(PromptView v,
+                                                                                                   SeqLens lens) {
+    constexpr int KS = D / (4 * kVec<T>), SUB = kStage / 16 / KW, HALVES = Staged<T, D>::HALVES;
+    constexpr int WG_ROWS = 16 * RT * (kWaves / KW);
+    __shared__ __align__(16) u32x4 s_k[HALVES][kStage * D / kVec<T>];
+    __shared__ float s_m[KW][WG_ROWS], s_l[KW][WG_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
     const int unit = blockIdx.x, b = v.seq0 + unit / v.nkv, h = unit % v.nkv, chunk = blockIdx.z;
     const int len = lens.len[unit / v.nkv], nq = seq_rows(v, len), rows = nq * v.G;
-    constexpr int WG_ROWS = 16 * RT * (ROWS ? kWaves : 1);
     const int wg0 = (gridDim.y - 1 - blockIdx.y) * WG_ROWS;
     if (wg0 >= rows) return;
-    const int r0 = wg0 + (ROWS ? w * 16 * RT : 0), lo = chunk * v.chunk_keys;
+    const int wk = w % KW, rw = w / KW * 16 * RT, r0 = wg0 + rw, lo = chunk * v.chunk_keys;
     // keys that the workgroup's and this wavefront's last row see
     const int seen = len - nq + query_of(v, min(wg0 + WG_ROWS, rows) - 1) + 1, hi = min(seen, lo + v.chunk_keys);
     if (lo >= hi) return;
     const int mine = r0 < rows ? min(hi, len - nq + query_of(v, min(r0 + 16 * RT, rows) - 1) + 1) : 0;
     const int full = len - nq + query_of(v, min(r0, rows - 1));  // last key that every row of the wavefront sees
     u32x4 q[RT][KS];
-    int last[RT];  // last key that the row sees
     float m[RT], l[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int rr = min(r0 + 16 * t + col, rows - 1);
-        load_row<T, D>(query_row<T, D>(v, b, h, rr), true, a, q[t]);
-        last[t] = len - nq + query_of(v, rr);
-        m[t] = -INFINITY;
+        load_row<T, D>(query_row<T, D>(v, b, h, min(r0 + 16 * t + col, rows - 1)), true, a, q[t]);
+        m[t] = kNothing;
         l[t] = 0.0f;
     }
     const T* K = (const T*)v.k + ((size_t)b * v.nkv + h) * v.P * D;
     Staged<T, D> next;
     next.load(tid, [&](int r) { return K + (size_t)min(lo + r, len - 1) * D; });
-    for (int j0 = lo; j0 < hi; j0 += kStage) {
-        lds_barrier();
-        next.store(tid, s_k);
+    for (int j0 = lo, buf = 0; j0 < hi; j0 += kStage, buf = (buf + 1) % HALVES) {
+        next.store(tid, s_k[buf]);
         lds_barrier();
         if (j0 + kStage < hi) next.load(tid, [&](int r) { return K + (size_t)min(j0 + kStage + r, len - 1) * D; });
-        if (j0 >= mine) continue;
-        const int jw = j0 + (ROWS ? 0 : w * 16 * SUB);
+        const int jw = j0 + wk * 16 * SUB;
+        if (jw >= mine) continue;
         auto stage = [&](auto masked) {
             f32x4 x[RT][SUB];
 #pragma unroll
@@ -159,7 +164,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
             for (int c = 0; c < SUB; ++c) {
                 u32x4 k[KS];
-                Staged<T, D>::read(s_k, ROWS ? c : w * SUB + c, a, col, k);
+                Staged<T, D>::read(s_k[buf], wk * SUB + c, a, col, k);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -168,25 +173,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 if constexpr (masked) {
+                    const int last = len - nq + query_of(v, min(r0 + 16 * t + col, rows - 1));
 #pragma unroll
                     for (int c = 0; c < SUB; ++c)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            x[t][c][e] = jw + 16 * c + 4 * a + e <= last[t] ? x[t][c][e] : -INFINITY;
+                            x[t][c][e] = jw + 16 * c + 4 * a + e <= last ? x[t][c][e] : -INFINITY;
                 }
                 float mb = x[t][0][0];
 #pragma unroll
                 for (int c = 0; c < SUB; ++c)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mb = fmaxf(mb, x[t][c][e]);
-                const float mn = fmaxf(m[t], mb * v.scale_log2), ref = mn == -INFINITY ? 0.0f : mn;
+                const float mn = fmaxf(m[t], mb * v.scale_log2);
                 float add = 0.0f;
 #pragma unroll
                 for (int c = 0; c < SUB; ++c)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        add += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][c][e], v.scale_log2, -ref));
-                l[t] = __builtin_fmaf(l[t], __builtin_amdgcn_exp2f(m[t] - ref), add);
+                        add += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][c][e], v.scale_log2, -mn));
+                l[t] = __builtin_fmaf(l[t], __builtin_amdgcn_exp2f(m[t] - mn), add);
                 m[t] = mn;
             }
         };
@@ -196,30 +202,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        float M = max_groups(m[t]);
-        float ref = M == -INFINITY ? 0.0f : M;
-        float Z = sum_groups(l[t] * __builtin_amdgcn_exp2f(m[t] - ref));
-        if constexpr (!ROWS) {
+        const float M = max_groups(m[t]);
+        const float Z = sum_groups(l[t] * __builtin_amdgcn_exp2f(m[t] - M));
+        const int r = rw + 16 * t + col;
+        if constexpr (KW > 1) {
             if (a == 0) {
-                s_m[w][16 * t + col] = M;
-                s_l[w][16 * t + col] = Z;
+                s_m[wk][r] = M;
+                s_l[wk][r] = Z;
             }
         } else {
-            const int r = r0 + 16 * t + col;
-            if (a == 0 && r < rows) row_done(v, unit, b, h, r, chunk, M, Z);
+            if (a == 0 && wg0 + r < rows) row_done(v, unit, b, h, wg0 + r, chunk, M, Z);
         }
     }
-    if constexpr (!ROWS) {
-        __syncthreads();
-        const int r = r0 + tid;
-        if (tid < RT * 16 && r < rows) {
-            float M = -INFINITY, Z = 0.0f;
+    if constexpr (KW > 1) {
+        lds_barrier();
+        if (tid < WG_ROWS && wg0 + tid < rows) {
+            float M = kNothing, Z = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kWaves; ++i) M = fmaxf(M, s_m[i][tid]);
-            const float ref = M == -INFINITY ? 0.0f : M;
+            for (int i = 0; i < KW; ++i) M = fmaxf(M, s_m[i][tid]);
 #pragma unroll
-            for (int i = 0; i < kWaves; ++i) Z += s_l[i][tid] * __builtin_amdgcn_exp2f(s_m[i][tid] - ref);
-            row_done(v, unit, b, h, r, chunk, M, Z);
+            for (int i = 0; i < KW; ++i) Z += s_l[i][tid] * __builtin_amdgcn_exp2f(s_m[i][tid] - M);
+            row_done(v, unit, b, h, wg0 + tid, chunk, M, Z);
         }
     }
 }
@@ -227,15 +230,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 // Probabilities of a chunk of query rows, summed per key. Grid: units, key
 // tiles (the ones that most rows see first), row chunks. A wavefront holds kHeld
 // tiles of 16 keys; the rows pass through LDS with their log-sum-exp (base 2).
+// Bound as the kernel above.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_keys(PromptView v, SeqLens lens) {
-    constexpr int KS = D / (4 * kVec<T>), KT = kHeld<T>, SUB = kStage / 16;
-    __shared__ __align__(16) u32x4 s_q[kStage * D / kVec<T>];
-    __shared__ float s_lse[kStage];
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_keys(PromptView v,
+                                                                                                   SeqLens lens) {
+    constexpr int KS = D / (4 * kVec<T>), KT = kHeld<T>, SUB = kStage / 16, HALVES = Staged<T, D>::HALVES;
+    constexpr int WG_KEYS = kWaves * 16 * KT;
+    __shared__ __align__(16) u32x4 s_q[HALVES][kStage * D / kVec<T>];
+    __shared__ float s_lse[HALVES][kStage];
     const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
     const int unit = blockIdx.x, b = v.seq0 + unit / v.nkv, h = unit % v.nkv;
     const int len = lens.len[unit / v.nkv], nq = seq_rows(v, len), rows = nq * v.G;
-    const int wg0 = blockIdx.y * kWaves * 16 * KT, j0 = wg0 + w * 16 * KT;
+    const int wg0 = blockIdx.y * WG_KEYS, j0 = wg0 + w * 16 * KT;
     if (wg0 >= len) return;
     const T* K = (const T*)v.k + ((size_t)b * v.nkv + h) * v.P * D;
     u32x4 k[KT][KS];
@@ -258,10 +264,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     };
     const int start = max(lo, first) / kStage * kStage;
     if (start < hi) load(start);
-    for (int r0 = start; r0 < hi; r0 += kStage) {
-        lds_barrier();
-        next.store(tid, s_q);
-        if (tid < kStage) s_lse[tid] = lse;
+    for (int r0 = start, buf = 0; r0 < hi; r0 += kStage, buf = (buf + 1) % HALVES) {
+        next.store(tid, s_q[buf]);
+        if (tid < kStage) s_lse[buf][tid] = lse;
         lds_barrier();
         if (r0 + kStage < hi) load(r0 + kStage);
         if (r0 + kStage <= mine || j0 >= len) continue;
@@ -270,8 +275,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
             for (int c = 0; c < SUB; ++c) {
                 u32x4 q[KS];
-                Staged<T, D>::read(s_q, c, a, col, q);
-                const float off = s_lse[16 * c + col];
+                Staged<T, D>::read(s_q[buf], c, a, col, q);
+                const float off = s_lse[buf][16 * c + col];
                 const int last = masked ? len - nq + query_of(v, r0 + 16 * c + col) : 0;
                 f32x4 x[KT];
 #pragma unroll
@@ -300,8 +305,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float x = sum[t][e];
-#pragma unroll
-            for (int d = 8; d >= 1; d >>= 1) x += __shfl_xor(x, d);
+            x += dpp_f<0xB1>(x);
+            x += dpp_f<0x4E>(x);
+            x += dpp_f<0x141>(x);
+            x += dpp_f<0x140>(x);
             const int j = j0 + 16 * t + 4 * a + e;
             if (col == 0 && j < len) to[j] = x;
         }
@@ -318,43 +325,43 @@ __global__ __launch_bounds__(kThreads) void k_prompt_sum(PromptView v, SeqLens l
 
 template <typename T, int D>
 void launch_t(const PromptView& v, const SeqLens& lens, int most, hipStream_t s) {
-    const int units = v.nseq * v.nkv, rows = std::min(most, v.W) * v.G;
-    const int chunks = (most + v.chunk_keys - 1) / v.chunk_keys, key_step = kWaves * 16 * kHeld<T>;
-    auto go = [&](auto kernel, int step) {
-        hipLaunchKernelGGL(kernel, dim3(units, (rows + step - 1) / step, chunks), dim3(kThreads), 0, s, v, lens);
+    constexpr int H = kHeld<T>;
+    const int units = v.nseq * v.nkv, rows = std::min(most, v.W) * v.G, all = v.W * v.G;
+    const int chunks = (most + v.chunk_keys - 1) / v.chunk_keys;
+    // (the choice goes by the call's sizes, as the plan's does)
+    auto by_rows = [&](auto kernel, int step) {
+        hipLaunchKernelGGL(kernel, dim3(units, (rows + step - 1) / step, chunks), dim3(kWaves * 64), 0, s, v, lens);
     };
-    if (rows <= 16) go(k_prompt_rows<T, D, 1, false>, 16);
-    else if (rows <= 16 * kHeld<T>) go(k_prompt_rows<T, D, kHeld<T>, false>, 16 * kHeld<T>);
-    else go(k_prompt_rows<T, D, kHeld<T>, true>, 16 * kHeld<T> * kWaves);
+    if (all <= 16) by_rows(k_prompt_rows<T, D, 1, 4>, 16);
+    else if (all <= 16 * H) by_rows(k_prompt_rows<T, D, H, 4>, 16 * H);
+    else by_rows(k_prompt_rows<T, D, H, 1>, 64 * H);
     if (v.chunks > 1)
         hipLaunchKernelGGL(k_prompt_join, dim3((rows + kThreads - 1) / kThreads, units), dim3(kThreads), 0, s, v, lens);
-    hipLaunchKernelGGL((k_prompt_keys<T, D>), dim3(units, (most + key_step - 1) / key_step, v.row_chunks),
-                       dim3(kThreads), 0, s, v, lens);
+    hipLaunchKernelGGL((k_prompt_keys<T, D>), dim3(units, (most + 64 * H - 1) / (64 * H), v.row_chunks),
+                       dim3(kWaves * 64), 0, s, v, lens);
     if (v.row_chunks > 1)
         hipLaunchKernelGGL(k_prompt_sum, dim3((most + kThreads - 1) / kThreads, units), dim3(kThreads), 0, s, v, lens);
 }
-
-}  // namespace
 
 // Workgroups wanted in each of the two kernels: about six per CU, so that the
 // causal part's uneven ones even out.
 constexpr int kWorkgroups = 1536;
 
+}  // namespace
+
 PromptPlan plan_prompt(int units, int G, int W, int P, bool bf16) {
     const int held = bf16 ? kHeld<uint16_t> : kHeld<float>;
-    const long long rows = (long long)W * G, row_step = rows <= 16 ? 16 : 16LL * held * (rows <= 16 * held ? 1 : kWaves);
-    const long long row_wgs = units * ((rows + row_step - 1) / row_step);
-    const long long key_wgs = units * (((long long)P + kWaves * 16 * held - 1) / (kWaves * 16 * held));
-    PromptPlan p;
+    const long long rows = (long long)W * G;
     // at least 512 keys or rows a piece
-    const long long want = std::min<long long>(kWorkgroups / row_wgs, P / 512);
-    p.chunks = (int)std::max<long long>(1, want);
-    p.chunk_keys = (int)(((P + p.chunks - 1) / p.chunks + kStage - 1) / kStage * kStage);
-    p.chunks = (P + p.chunk_keys - 1) / p.chunk_keys;
-    const long long want_rows = std::min<long long>(kWorkgroups / key_wgs, rows / 512);
-    p.row_chunks = (int)std::max<long long>(1, want_rows);
-    p.chunk_rows = (int)(((rows + p.row_chunks - 1) / p.row_chunks + kStage - 1) / kStage * kStage);
-    p.row_chunks = (int)((rows + p.chunk_rows - 1) / p.chunk_rows);
+    auto pieces = [&](long long n, long long others, long long tile, int& count, int& size) {
+        const long long wgs = units * ((others + tile - 1) / tile);
+        const long long want = std::max(1LL, std::min<long long>(kWorkgroups / wgs, n / 512));
+        size = (int)(((n + want - 1) / want + kStage - 1) / kStage * kStage);
+        count = (int)((n + size - 1) / size);
+    };
+    PromptPlan p;
+    pieces(P, rows, rows <= 16 ? 16 : rows <= 16 * held ? 16 * held : 64 * held, p.chunks, p.chunk_keys);
+    pieces(rows, P, 64 * held, p.row_chunks, p.chunk_rows);
     return p;
 }
 

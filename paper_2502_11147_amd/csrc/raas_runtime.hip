@@ -303,17 +303,25 @@ raas_status static_scratch(void** out) {
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Bytes of keys and values that this process's steps have read, per device: a
-// hint that chooses between two kinds of load. Both read the same values; their
+// What count_streamed counts. Both kinds of load read the same values; the step's
 // kernel instances may round an output differently, as the dynamic claims do.
 std::atomic<unsigned long long> g_streamed[kMaxDevices];
 
-bool capturing(hipStream_t s) {
+}  // namespace
+
+unsigned long long raas::count_streamed(int device, unsigned long long bytes) {
+    if (device < 0 || device >= kMaxDevices) device = 0;  // (only picks a counter)
+    return g_streamed[device].fetch_add(bytes, std::memory_order_relaxed);
+}
+
+bool raas::capturing(hipStream_t s) {
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
     if (s == nullptr) return false;  // (the legacy stream cannot be captured)
     if (hipStreamIsCapturing(s, &st) != hipSuccess) (void)hipGetLastError();
     return st != hipStreamCaptureStatusNone;
 }
+
+namespace {
 
 // The load kind of a step. A layer's first step
 // counts the pool's other layers; a deterministic pool always does, so that its

@@ -65,17 +65,16 @@ struct WeightPlan {
     int waves;    // wavefronts per workgroup
     int nsplit;   // workgroups per unit
     bool fused;   // one workgroup per unit, which keeps the logits in LDS
-    bool stream;  // keys and values are read with non-temporal loads
 };
-// layer_bytes: keys and values of the layers that are stepped in turn
-WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16, double layer_bytes);
+WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16);
 hipError_t weight_allow_lds(bool bf16, int D, int waves);
 // Chooses the kept tokens of each selected unit and writes its records, then
 // stores their keys and values. Sequences seq0 .. seq0 + nseq - 1.
 hipError_t launch_weight_prefill(const WeightView& L, bool bf16, const void* k, const void* v, const float* weights,
                                  const SeqLens& lens, int seq0, int nseq, int max_len, hipStream_t s);
+// stream: keys and values are read with non-temporal loads
 hipError_t launch_weight_step(const WeightView& L, bool bf16, const WeightStepIO& io, const WeightPlan& plan,
-                              hipStream_t s);
+                              bool stream, hipStream_t s);
 
 // One layer of a shared prefix: K, V [nkv][tpad][D] in blocks.
 struct PrefixView {

@@ -43,25 +43,20 @@ struct Lightest {
 };
 
 // Over a workgroup of NT threads; the result is valid on thread 0. Positions
-// of a unit differ, so no two keys are equal.
+// of a unit differ, so no two keys are equal (but those of no token).
 template <int NT>
 __device__ __forceinline__ Lightest lightest_wg(Lightest b, int tid) {
     __shared__ unsigned long long s_key[NT / 64];
     __shared__ int s_place[NT / 64];
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        const unsigned long long k = __shfl_xor(b.key, d);
-        const int p = __shfl_xor(b.place, d);
-        b.take(k, p);
-    }
-    if ((tid & 63) == 0) {
-        s_key[tid >> 6] = b.key;
+    const unsigned long long least = wave_min(b.key);
+    if (b.key == least && (b.place >= 0 || (tid & 63) == 0)) {
+        s_key[tid >> 6] = least;
         s_place[tid >> 6] = b.place;
     }
-    __syncthreads();
+    lds_barrier();
     if (tid == 0)
 #pragma unroll
-        for (int i = 1; i < NT / 64; ++i) b.take(s_key[i], s_place[i]);
+        for (int i = 0; i < NT / 64; ++i) b.take(s_key[i], s_place[i]);
     return b;
 }
 
@@ -102,7 +97,7 @@ __device__ __forceinline__ int rank_wg(bool flag, int tid, int* s_n, int& total)
 
 __global__ __launch_bounds__(kSelectThreads) void k_weight_select(WeightView L, const float* __restrict__ weights,
                                                                   SeqLens lens, int seq0, int max_len) {
-    __shared__ int s_hist[256], s_pick[2], s_a[kSelectThreads / 64], s_b[kSelectThreads / 64];
+    __shared__ int s_hist[256], s_pick[3], s_a[kSelectThreads / 64], s_b[kSelectThreads / 64];
     const int tid = threadIdx.x, P = lens.len[blockIdx.x / L.nkv];
     if (P < 0) return;  // not selected
     const int u = seq0 * L.nkv + blockIdx.x, C = L.C;
@@ -133,17 +128,35 @@ __global__ __launch_bounds__(kSelectThreads) void k_weight_select(WeightView L, 
                 if ((key & high) == cut) atomicAdd(&s_hist[(key >> shift) & 255u], 1);
             }
             __syncthreads();
-            if (tid == 0) {
-                int b = 255, left = want;
-                while (b > 0 && s_hist[b] < left) left -= s_hist[b--];
-                s_pick[0] = b;
-                s_pick[1] = left;
+            if (tid < 64) {  // lane l: bins 255 - 4 l and the three below, from the top
+                int n[4], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += n[i] = s_hist[255 - 4 * tid - i];
+                int upto = sum;  // keys in this lane's bins and all above
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int y = __shfl_up(upto, d);
+                    if (tid >= d) upto += y;
+                }
+                int left = want - (upto - sum);  // rank from the top within this lane's bins
+                if (left > 0 && left <= sum) {
+                    int i = 0, held = n[0];
+#pragma unroll
+                    for (int k = 1; k < 4; ++k)
+                        if (i == k - 1 && left > held) {
+                            left -= held;
+                            i = k;
+                            held = n[k];
+                        }
+                    s_pick[0] = 255 - 4 * tid - i;
+                    s_pick[1] = left;
+                    s_pick[2] = held;
+                }
             }
             __syncthreads();
             cut |= (uint32_t)s_pick[0] << shift;
             want = s_pick[1];
-            equal = s_hist[s_pick[0]];
-            __syncthreads();
+            equal = s_pick[2];
         }
         const int skip = equal - want;  // the oldest of the tokens at the cut go
         int kept = 0, ties = 0;
@@ -263,24 +276,38 @@ typedef int32_t i32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
+// Positions and weights of four tokens.
+struct Records {
+    i32x4 p = {0, 0, 0, 0};
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void load(const WeightView& L, int u, int j, int n) {
+        if (j >= n) return;
+        p = *reinterpret_cast<const i32x4*>(L.pos + (size_t)u * L.cpad + j);
+        w = *reinterpret_cast<const f32x4*>(L.w + (size_t)u * L.cpad + j);
+    }
+};
+
+// `now`: the records of this thread's first tokens, 4 tid + i STEP on, which the
+// caller has had on their way for a while. (All of a group's reads come before
+// its first write: a wait for a read that follows a write waits for the write.)
+constexpr int kRecords = 4;
+template <int NW>
+__device__ __forceinline__ void load_records(const WeightView& L, int u, int j, int n, Records (&now)[kRecords]) {
+#pragma unroll
+    for (int i = 0; i < kRecords; ++i) now[i].load(L, u, j + i * NW * 256, n);
+}
+
 template <typename T, int D, int NW, class Ml, class O, class X4>
 __device__ __forceinline__ void finish_step(const WeightView& L, const WeightStepIO& io, int u, const int4& rec,
-                                            int nsrc, float* s_w, Ml ml, O o, X4 x4) {
+                                            int tid, Records (&now)[kRecords], int nsrc, float* s_w, Ml ml, O o, X4 x4) {
     constexpr int NT = NW * 64, STEP = NT * 4;
     __shared__ float s_m[16], s_rz[16];
-    const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), G = L.G, C = L.C;
+    const int lane = tid & 63, w = wave_of(tid), G = L.G, C = L.C;
     const PrefixParts& pp = io.prefix;
     const size_t rows = (size_t)L.nkv * pp.rows, row0 = (size_t)(u % L.nkv) * pp.rows + (size_t)(u / L.nkv) * G;
-    const int now = rec.y, place = rec.z, n = min(rec.x + 1, C), before = now + 1 - L.recent;
+    const int clock = rec.y, place = rec.z, n = min(rec.x + 1, C), before = clock + 1 - L.recent;
     int32_t* pos = L.pos + (size_t)u * L.cpad;
     float* wt = L.w + (size_t)u * L.cpad;
-    // the first tokens' records travel while the parts are joined
-    i32x4 p4 = {0, 0, 0, 0};
-    f32x4 w4 = {0.f, 0.f, 0.f, 0.f};
-    if (4 * tid < n) {
-        p4 = *reinterpret_cast<const i32x4*>(pos + 4 * tid);
-        w4 = *reinterpret_cast<const f32x4*>(wt + 4 * tid);
-    }
     const int parts = nsrc + pp.n;
     for (int g = w; g < G; g += NW) {
         auto part_ml = [&](int s) {
@@ -292,15 +319,13 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
         const float2 first = lane < parts ? part_ml(lane) : make_float2(-INFINITY, 0.0f);
         M = first.x;
         for (int s = lane + 64; s < parts; s += 64) M = fmaxf(M, part_ml(s).x);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+        M = wave_max(M);
         Z = first.y * __builtin_amdgcn_exp2f(first.x - M);
         for (int s = lane + 64; s < parts; s += 64) {
             const float2 y = part_ml(s);
             Z += y.y * __builtin_amdgcn_exp2f(y.x - M);
         }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) Z += __shfl_xor(Z, d);
+        Z = wave_sum(Z);
         const float rz = 1.0f / Z;
         if (lane < parts) s_w[lane * G + g] = __builtin_amdgcn_exp2f(first.x - M) * rz;
         for (int s = lane + 64; s < parts; s += 64) s_w[s * G + g] = __builtin_amdgcn_exp2f(part_ml(s).x - M) * rz;
@@ -309,116 +334,115 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
             s_rz[g] = rz;
         }
     }
-    __syncthreads();
+    lds_barrier();
     for (int i = tid; i < G * D; i += NT) {
         const int g = i / D, c = i % D;
         float x = 0.0f;
-#pragma unroll 8
+#pragma unroll 4
         for (int s = 0; s < nsrc; ++s) x += o(s, g, c) * s_w[s * G + g];
-#pragma unroll 8
+#pragma unroll 4
         for (int s = 0; s < pp.n; ++s) x += pp.o[(s * rows + row0 + g) * D + c] * s_w[(nsrc + s) * G + g];
         ((T*)io.out)[((size_t)u * G + g) * D + c] = from_f<T>(x);
     }
     Lightest best;
-    for (int j = 4 * tid; j < C; j += STEP) {
-        if (j >= n && io.positions_out == nullptr && io.weights_out == nullptr) break;
-        if (j > 4 * tid && j < n) {
-            p4 = *reinterpret_cast<const i32x4*>(pos + j);
-            w4 = *reinterpret_cast<const f32x4*>(wt + j);
-        }
-        f32x4 a = {0.f, 0.f, 0.f, 0.f};
-        if (j < n) {
+    const int end = io.positions_out != nullptr || io.weights_out != nullptr ? C : n;
+    for (int j0 = 4 * tid; j0 < end; j0 += kRecords * STEP) {
+        if (j0 > 4 * tid) load_records<NW>(L, u, j0, n, now);
+#pragma unroll
+        for (int i = 0; i < kRecords; ++i) {
+            const int j = j0 + i * STEP;
+            if (j >= end) break;
+            f32x4 a = {0.f, 0.f, 0.f, 0.f};
+            if (j < n) {
 #pragma unroll 4
-            for (int g = 0; g < G; ++g) {
-                const f32x4 x = x4(g, j);
-                const float M = s_m[g], rz = s_rz[g];
+                for (int g = 0; g < G; ++g) {
+                    const f32x4 x = x4(g, j);
+                    const float M = s_m[g], rz = s_rz[g];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - M), rz, a[e]);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool fresh = j + e == place, held = j + e < n;
-            p4[e] = fresh ? now : held ? p4[e] : -1;
-            w4[e] = held ? (fresh ? 0.0f : w4[e]) + a[e] : 0.0f;
-            if (held && p4[e] < before) best.offer(w4[e], p4[e], j + e);
-        }
-        if (j < n) {
-            *reinterpret_cast<f32x4*>(wt + j) = w4;
-            if (place >= j && place < j + 4) pos[place] = now;
-        }
-        if (j + 4 <= C) {
-            if (io.positions_out) *reinterpret_cast<i32x4_at4*>(io.positions_out + (size_t)u * C + j) = p4;
-            if (io.weights_out) *reinterpret_cast<f32x4_at4*>(io.weights_out + (size_t)u * C + j) = w4;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (j + e < C) {
-                    if (io.positions_out) io.positions_out[(size_t)u * C + j + e] = p4[e];
-                    if (io.weights_out) io.weights_out[(size_t)u * C + j + e] = w4[e];
+                    for (int e = 0; e < 4; ++e) a[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - M), rz, a[e]);
                 }
+            }
+            i32x4& p4 = now[i].p;
+            f32x4& w4 = now[i].w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool fresh = j + e == place, held = j + e < n;
+                p4[e] = fresh ? clock : held ? p4[e] : -1;
+                w4[e] = held ? (fresh ? 0.0f : w4[e]) + a[e] : 0.0f;
+                if (held && p4[e] < before) best.offer(w4[e], p4[e], j + e);
+            }
+            if (j < n) {
+                *reinterpret_cast<f32x4*>(wt + j) = w4;
+                if (place >= j && place < j + 4) pos[place] = clock;
+            }
+            if (j + 4 <= C) {
+                if (io.positions_out) *reinterpret_cast<i32x4_at4*>(io.positions_out + (size_t)u * C + j) = p4;
+                if (io.weights_out) *reinterpret_cast<f32x4_at4*>(io.weights_out + (size_t)u * C + j) = w4;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (j + e < C) {
+                        if (io.positions_out) io.positions_out[(size_t)u * C + j + e] = p4[e];
+                        if (io.weights_out) io.weights_out[(size_t)u * C + j + e] = w4[e];
+                    }
+            }
         }
     }
     if (n == C) best = lightest_wg<NT>(best, tid);
     if (tid == 0) {
         if (io.evicted_out) io.evicted_out[u] = rec.w;
-        write_unit(L, u, n, now + 1, best);
+        write_unit(L, u, n, clock + 1, best);
     }
 }
 
 // ---------------------------------------------------------------------------
-// The step: one workgroup of NW wavefronts per (unit, split). Split s of a unit
-// takes every nsplit-th block, a wavefront every NW-th of those, so the order of
-// every sum is fixed and the work is even however many tokens are held; a block
-// is read while the one before it is attended to. The new token's row is
-// replaced in registers by the wavefront that holds its block, which stores it.
-// FUSED: one workgroup covers the unit and keeps the logits in LDS; else the
-// last of the unit's workgroups to end finishes the step from what all of them
-// published. STREAM: the layer does not stay in the memory-side cache.
+// The step. Split s of a unit takes every nsplit-th block, a wavefront every
+// NW-th of those, so the order of every sum is fixed and the work is even
+// however many tokens are held; a block is read while the one before it is
+// attended to. The new token's row is replaced in registers by the wavefront
+// that holds its block, which stores it. Bound by memory: 32 KB per wavefront
+// are on their way or in use.
+// FUSED: one workgroup covers a unit and keeps the logits in LDS. Else one per
+// (unit, split), and the last of a unit's to end finishes the step from what all
+// of them published. STREAM: non-temporal loads.
 template <typename T, int D, int NW, bool FUSED, bool STREAM>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_weight_step(WeightView L,
                                                                                                  WeightStepIO io) {
     constexpr int VE = kVec<T>, BT = kTokens<T>, QT = kTiles<T>, KS = D / (4 * VE), NP = D / 16;
     extern __shared__ __align__(16) float smem[];
     const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
-    const int u = FUSED ? blockIdx.x : blockIdx.x / L.nsplit, split = FUSED ? 0 : blockIdx.x - u * L.nsplit;
-    const int nsplit = FUSED ? 1 : L.nsplit;
-    if (io.active != nullptr && io.active[u / L.nkv] == 0) return;  // the sequence sits this step out
-    const int G = L.G;
+    const int G = L.G, nsplit = FUSED ? 1 : L.nsplit, last_block = L.cpad / BT - 1, step = NW * nsplit;
     float* s_ml = smem;                    // [NW][16][2]
     float* s_w = s_ml + NW * 32;           // [parts][G], 16-byte multiple
     float* s_o = s_w + L.wfloats;          // [NW][G][D + 4]
     float* s_x = s_o + NW * G * (D + 4);   // [G][cpad], fused only
-    T* Ku = (T*)L.K + (size_t)u * L.cpad * D;
-    T* Vu = (T*)L.V + (size_t)u * L.cpad * D;
-    const int last_block = L.cpad / BT - 1, step = NW * nsplit;
+    const int u = FUSED ? blockIdx.x : blockIdx.x / nsplit, split = FUSED ? 0 : blockIdx.x - u * nsplit;
+    if (io.active != nullptr && io.active[u / L.nkv] == 0) return;  // the sequence sits this step out
 
-    u32x4 k0[NP], v0[NP], k1[NP], v1[NP];
+    u32x4 k0[NP], v0[NP], k1[NP], v1[NP], q[KS];
     auto load = [&](int b, u32x4 (&kr)[NP], u32x4 (&vr)[NP]) {
-        const size_t at = (size_t)min(b, last_block) * BT * D + lane * VE;
+        const size_t at = ((size_t)u * L.cpad + (size_t)min(b, last_block) * BT) * D + lane * VE;
+        const T *Kb = (const T*)L.K + at, *Vb = (const T*)L.V + at;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) kr[i] = STREAM ? ld16_nt(Ku + at + i * 64 * VE) : ld16(Ku + at + i * 64 * VE);
+        for (int i = 0; i < NP; ++i) kr[i] = STREAM ? ld16_nt(Kb + i * 64 * VE) : ld16(Kb + i * 64 * VE);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) vr[i] = STREAM ? ld16_nt(Vu + at + i * 64 * VE) : ld16(Vu + at + i * 64 * VE);
+        for (int i = 0; i < NP; ++i) vr[i] = STREAM ? ld16_nt(Vb + i * 64 * VE) : ld16(Vb + i * 64 * VE);
     };
     // (the first block's place does not depend on the record, which arrives meanwhile)
-    int b = split + nsplit * w;
-    load(b, k0, v0);
+    load(split + nsplit * w, k0, v0);
     const int4 rec = *reinterpret_cast<const int4*>(L.unit + (size_t)u * kWeightFields);
-    const T* kn = (const T*)io.k_new + (size_t)u * D;
-    const T* vn = (const T*)io.v_new + (size_t)u * D;
-    u32x4 q[KS];
     load_row<T, D>((const T*)io.q + ((size_t)u * G + col) * D, col < G, a, q);
     const int n = min(rec.x + 1, L.C), nb = (n + BT - 1) / BT;
     const int tail = rec.z / BT;  // the block that the new token goes to
     float* xs = FUSED ? s_x : L.logits + (size_t)u * G * L.cpad;
     Softmax<D> s;
     s.clear();
-
     auto block = [&](int b, u32x4 (&kr)[NP], u32x4 (&vr)[NP]) {
         if (b == tail) {
+            const T* kn = (const T*)io.k_new + (size_t)u * D;
+            const T* vn = (const T*)io.v_new + (size_t)u * D;
             const int t = rec.z - b * BT, e = t % VE;
-            const size_t at = (size_t)b * BT * D + lane * VE;
+            const size_t at = ((size_t)u * L.cpad + (size_t)b * BT) * D + lane * VE;
             if (col == 4 * (t / VE) + t % 4) {
 #pragma unroll
                 for (int qq = 0; qq < QT; ++qq)
@@ -426,7 +450,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
                             kr[qq * KS + ks] = ld16_in<T>(kn + 4 * VE * ks + VE * a);
-                            st16(Ku + at + (qq * KS + ks) * 64 * VE, kr[qq * KS + ks]);
+                            st16((T*)L.K + at + (qq * KS + ks) * 64 * VE, kr[qq * KS + ks]);
                         }
             }
             if (a == t / VE) {
@@ -436,7 +460,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
                     for (int ee = 0; ee < VE; ++ee)
                         if (ee == e) set_elem<T>(vr[ct], ee, x);
-                    st16(Vu + at + ct * 64 * VE, vr[ct]);
+                    st16((T*)L.V + at + ct * 64 * VE, vr[ct]);
                 }
             }
         }
@@ -455,17 +479,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 else publish4(to, x[t]);
             }
     };
-    if (b < nb) {
-        while (true) {
-            load(b + step, k1, v1);
-            block(b, k0, v0);
-            b += step;
-            if (b >= nb) break;
-            load(b + step, k0, v0);
-            block(b, k1, v1);
-            b += step;
-            if (b >= nb) break;
-        }
+    for (int b = split + nsplit * w; b < nb;) {
+        load(b + step, k1, v1);
+        block(b, k0, v0);
+        b += step;
+        if (b >= nb) break;
+        load(b + step, k0, v0);
+        block(b, k1, v1);
+        b += step;
     }
     s.l = sum_groups(s.l);
     if (col < G) {
@@ -477,12 +498,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int ct = 0; ct < NP; ++ct)
             *reinterpret_cast<f32x4*>(s_o + (size_t)(w * G + col) * (D + 4) + 16 * ct + 4 * a) = s.o[ct];
     }
-    __syncthreads();
+    Records first[kRecords];
+    if constexpr (FUSED) load_records<NW>(L, u, 4 * tid, n, first);
+    lds_barrier();
     auto ml = [&](int i, int g) { return make_float2(s_ml[2 * (i * 16 + g)], s_ml[2 * (i * 16 + g) + 1]); };
     auto o = [&](int i, int g, int c) { return s_o[(size_t)(i * G + g) * (D + 4) + c]; };
     if constexpr (FUSED) {
         auto x4 = [&](int g, int j) { return *reinterpret_cast<const f32x4*>(s_x + (size_t)g * L.cpad + j); };
-        finish_step<T, D, NW>(L, io, u, rec, NW, s_w, ml, o, x4);
+        finish_step<T, D, NW>(L, io, u, rec, tid, first, NW, s_w, ml, o, x4);
     } else {
         float* mlp = L.ml + (size_t)u * nsplit * G * 2;
         float* part = L.part + (size_t)u * nsplit * G * D;
@@ -505,17 +528,21 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
             }
         }
         if (!arrive_last(L.arrived + u, nsplit)) return;
+        load_records<NW>(L, u, 4 * tid, n, first);
         auto gml = [&](int i, int g) {
             return make_float2(published(mlp + 2 * (i * G + g)), published(mlp + 2 * (i * G + g) + 1));
         };
         auto go = [&](int i, int g, int c) { return published(part + (size_t)(i * G + g) * D + c); };
         auto x4 = [&](int g, int j) { return published4(xs + (size_t)g * L.cpad + j); };
-        finish_step<T, D, NW>(L, io, u, rec, nsplit, s_w, gml, go, x4);
+        finish_step<T, D, NW>(L, io, u, rec, tid, first, nsplit, s_w, gml, go, x4);
     }
 }
 
 // Floats of the parts' shares: those of the workgroup's wavefronts or splits, and of the prefix.
 int share_floats(int G, int parts) { return (G * parts + 3) / 4 * 4; }
+
+// The fixed part of a step's workgroup in the time of a block, and of a split unit's.
+constexpr int kFusedBlocks = 8, kSplitBlocks = 20;
 
 size_t step_lds(int G, int D, int cpad, int nw, bool fused, int parts) {
     return sizeof(float) * ((size_t)nw * 32 + share_floats(G, parts) + (size_t)nw * G * (D + 4) +
@@ -523,12 +550,13 @@ size_t step_lds(int G, int D, int cpad, int nw, bool fused, int parts) {
 }
 
 template <typename T, int D, int NW>
-hipError_t launch_step_t(const WeightView& L, const WeightStepIO& io, const WeightPlan& p, size_t lds, hipStream_t s) {
+hipError_t launch_step_t(const WeightView& L, const WeightStepIO& io, const WeightPlan& p, bool stream, size_t lds,
+                         hipStream_t s) {
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)L.U * p.nsplit), dim3(NW * 64), lds, s, L, io);
         return hipGetLastError();
     };
-    if (p.stream) return p.fused ? go(k_weight_step<T, D, NW, true, true>) : go(k_weight_step<T, D, NW, false, true>);
+    if (stream) return p.fused ? go(k_weight_step<T, D, NW, true, true>) : go(k_weight_step<T, D, NW, false, true>);
     return p.fused ? go(k_weight_step<T, D, NW, true, false>) : go(k_weight_step<T, D, NW, false, false>);
 }
 
@@ -562,19 +590,33 @@ void launch_store(int D, bool bf16, void* K, void* V, const void* k, const void*
 
 }  // namespace
 
-WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16, double layer_bytes) {
+WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16) {
     const int bt = bf16 ? 32 : 16, nb = (C + bt - 1) / bt, cpad = nb * bt;
     WeightPlan p{};
     auto fits = [&](int nw, int per_cu) {
         return per_cu * (step_lds(G, D, cpad, nw, true, nw + kMaxPrefixParts) + 1024) <= kStepLds;
     };
     p.waves = 8;
+    // more units than CUs: two workgroups of 4 wavefronts per CU, so that one
+    // unit's finish overlaps another's reads
     if (U > 256 && fits(4, 2)) p.waves = 4;
     if (step_lds(G, D, cpad, 8, false, kMaxStepSplits + kMaxPrefixParts) > kStepLds) p.waves = 4;
-    const int want = U >= 192 || nb <= 32 ? 1 : std::min({512 / U, (nb + p.waves - 1) / p.waves, kMaxStepSplits});
-    p.fused = want <= 1 && fits(p.waves, 1);
-    p.nsplit = std::max(want, 1);
-    p.stream = layer_bytes > 300e6;
+    // Splits: the number that ends soonest when `per` workgroups run at a time
+    // and each takes a fixed part (more of it when the unit is split) besides its
+    // blocks, in units of one block at full load.
+    const int per = p.waves == 8 ? 256 : 512;
+    int want = 1;
+    double best = 0.0;
+    for (int ns = 1; ns <= kMaxStepSplits && (ns == 1 || nb >= ns * p.waves); ++ns) {
+        const double rounds = ((long long)U * ns + per - 1) / per;
+        const double cost = rounds * ((nb + ns - 1) / ns + (ns > 1 ? kSplitBlocks : kFusedBlocks));
+        if (ns == 1 || cost < best) {
+            best = cost;
+            want = ns;
+        }
+    }
+    p.fused = want == 1 && fits(p.waves, 1);
+    p.nsplit = want;
     return p;
 }
 
@@ -599,7 +641,7 @@ hipError_t launch_weight_prefill(const WeightView& L, bool bf16, const void* k, 
 }
 
 hipError_t launch_weight_step(const WeightView& view, bool bf16, const WeightStepIO& io, const WeightPlan& p,
-                              hipStream_t s) {
+                              bool stream, hipStream_t s) {
     WeightView L = view;
     const int parts = (p.fused ? p.waves : p.nsplit) + io.prefix.n;
     L.wfloats = share_floats(L.G, parts);
@@ -607,9 +649,10 @@ hipError_t launch_weight_step(const WeightView& view, bool bf16, const WeightSte
     auto go = [&](auto w) {
         constexpr int NW = decltype(w)::value;
         if (bf16)
-            return L.D == 128 ? launch_step_t<uint16_t, 128, NW>(L, io, p, lds, s)
-                              : launch_step_t<uint16_t, 64, NW>(L, io, p, lds, s);
-        return L.D == 128 ? launch_step_t<float, 128, NW>(L, io, p, lds, s) : launch_step_t<float, 64, NW>(L, io, p, lds, s);
+            return L.D == 128 ? launch_step_t<uint16_t, 128, NW>(L, io, p, stream, lds, s)
+                              : launch_step_t<uint16_t, 64, NW>(L, io, p, stream, lds, s);
+        return L.D == 128 ? launch_step_t<float, 128, NW>(L, io, p, stream, lds, s)
+                          : launch_step_t<float, 64, NW>(L, io, p, stream, lds, s);
     };
     return p.waves == 8 ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 4>{});
 }

@@ -105,6 +105,7 @@ struct raas_weight_cache {
     float *w = nullptr, *logits = nullptr, *part = nullptr, *ml = nullptr;
     size_t bytes = 0;
     std::vector<unsigned char> prefilled;
+    std::vector<unsigned long long> streamed_at;  // count_streamed after each layer's last step; 0: no step yet
     hipStream_t last_stream = nullptr;
 };
 
@@ -159,6 +160,12 @@ raas_status check_layer(const raas_prefix* p, int32_t layer) {
         return fail(RAAS_E_INVALID, "layer %d out of range [0, %d)", layer, p->cfg.n_layers);
     return RAAS_OK;
 }
+
+// Whether a step reads its layer of `own` bytes with non-temporal loads, which
+// leave the memory-side cache (256 MB) alone: where too little of the layer is
+// still there (us per step, ordinary / non-temporal, others' bytes in between:
+// NT_FIGURES).
+bool non_temporal(double own, double others) { return others + own * 2.0 / 3.0 > 256e6; }
 
 // The prefix's attention of `rows` sequences' queries into its parts.
 raas_status prefix_parts(raas_prefix* p, int32_t layer, const void* q, int rows, PrefixView& P, hipStream_t s) {
@@ -219,6 +226,7 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
     try {
         c = new raas_weight_cache();
         c->prefilled.assign((size_t)cfg->n_layers, 0);
+        c->streamed_at.assign((size_t)cfg->n_layers, 0);
         c->cfg = *cfg;
         c->bf16 = cfg->dtype == RAAS_BF16;
         c->U = cfg->batch * cfg->n_kv_heads;
@@ -226,7 +234,7 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
         c->C = cfg->capacity;
         c->cpad = pad_tokens(cfg->capacity, c->bf16);
         const size_t Ly = (size_t)cfg->n_layers, U = (size_t)c->U, d = (size_t)cfg->head_dim, esz = c->bf16 ? 2 : 4;
-        c->plan = plan_weight_step(c->U, c->G, cfg->head_dim, c->C, c->bf16, 2.0 * Ly * U * c->cpad * d * esz);
+        c->plan = plan_weight_step(c->U, c->G, cfg->head_dim, c->C, c->bf16);
         hipError_t e = hipGetDevice(&c->device);
         if (e == hipSuccess) e = weight_allow_lds(c->bf16, cfg->head_dim, c->plan.waves);
         if (e != hipSuccess) {
@@ -337,7 +345,19 @@ raas_status raas_weight_step(raas_weight_cache* c, int32_t layer, const void* q,
         if (st != RAAS_OK) return st;
         io.prefix = PrefixParts{P.part, P.ml, P.nsplit, P.rows};
     }
-    const hipError_t e = launch_weight_step(view(c, layer), c->bf16, io, c->plan, s);
+    // What other layers, caches and pools have read since the layer's last step
+    // decides whether it is still in the memory-side cache; a captured step, whose
+    // replays are not seen here, counts the cache's other layers.
+    const double own = 2.0 * c->U * c->cpad * c->cfg.head_dim * (c->bf16 ? 2 : 4);
+    const bool captured = capturing(s);
+    double others = (c->cfg.n_layers - 1.0) * own;
+    if (!captured) {
+        const unsigned long long before = count_streamed(c->device, (unsigned long long)own);
+        if (c->streamed_at[layer] != 0) others = (double)(before - c->streamed_at[layer]);
+        c->streamed_at[layer] = before + (unsigned long long)own;
+    }
+    const hipError_t e =
+        launch_weight_step(view(c, layer), c->bf16, io, c->plan, non_temporal(own, others), s);
     if (e != hipSuccess) return hip_fail(e, "step launch");
     c->last_stream = s;
     return RAAS_OK;
