@@ -35,6 +35,8 @@ struct WeightView {
     int32_t* arrived;  // [U] splits of the unit that have published; zero between launches
     int U, G, D, C, cpad, nkv, recent, nsplit;
     int wfloats;   // LDS floats of the parts' shares
+    int finish_parts;  // workgroups per unit of the kernel that ends a step, 0: none
+    unsigned long long* best;  // [U][finish_parts][2] key and place of each one's lightest token
     float scale_log2;
 };
 
@@ -65,6 +67,7 @@ struct WeightPlan {
     int waves;    // wavefronts per workgroup
     int nsplit;   // workgroups per unit
     bool fused;   // one workgroup per unit, which keeps the logits in LDS
+    int finish_parts;  // workgroups per unit of the kernel that ends a step, 0: the step kernel does
 };
 WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16);
 hipError_t weight_allow_lds(bool bf16, int D, int waves);

@@ -268,10 +268,11 @@ __device__ __forceinline__ bool arrive_last(int32_t* counter, int total) {
 // ---------------------------------------------------------------------------
 // The end of a step: from the maxima and sums (ml) and unnormalised outputs (o)
 // of `nsrc` disjoint parts of the held tokens, and those of the prefix, the
-// output; from the logits (x4: those of four tokens) the weights; the new
-// token's position; the lightest token. One workgroup of NW wavefronts; s_w:
-// [nsrc + prefix parts][G] floats of LDS. A wavefront per head finds the
-// maximum and the sum, a lane per part; a thread takes four tokens at a time.
+// output (if j_lo is 0); from the logits (x4: those of four tokens) the weights
+// of places j_lo .. j_hi - 1; the new token's position; the lightest token among
+// those places (thread 0's result). One workgroup of NW wavefronts; s_w: [nsrc +
+// prefix parts][G] floats of LDS. A wavefront per head finds the maximum and the
+// sum, a lane per part; a thread takes four tokens at a time.
 typedef int32_t i32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
@@ -287,7 +288,7 @@ struct Records {
     }
 };
 
-// `now`: the records of this thread's first tokens, 4 tid + i STEP on, which the
+// `now`: the records of this thread's first tokens, j_lo + 4 tid + i STEP on, which the
 // caller has had on their way for a while. (All of a group's reads come before
 // its first write: a wait for a read that follows a write waits for the write.)
 constexpr int kRecords = 4;
@@ -298,8 +299,9 @@ __device__ __forceinline__ void load_records(const WeightView& L, int u, int j, 
 }
 
 template <typename T, int D, int NW, class Ml, class O, class X4>
-__device__ __forceinline__ void finish_step(const WeightView& L, const WeightStepIO& io, int u, const int4& rec,
-                                            int tid, Records (&now)[kRecords], int nsrc, float* s_w, Ml ml, O o, X4 x4) {
+__device__ __forceinline__ Lightest finish_step(const WeightView& L, const WeightStepIO& io, int u, const int4& rec,
+                                            int tid, int j_lo, int j_hi, Records (&now)[kRecords], int nsrc,
+                                                float* s_w, Ml ml, O o, X4 x4) {
     constexpr int NT = NW * 64, STEP = NT * 4;
     __shared__ float s_m[16], s_rz[16];
     const int lane = tid & 63, w = wave_of(tid), G = L.G, C = L.C;
@@ -335,7 +337,7 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
         }
     }
     lds_barrier();
-    for (int i = tid; i < G * D; i += NT) {
+    for (int i = tid; i < (j_lo == 0 ? G * D : 0); i += NT) {
         const int g = i / D, c = i % D;
         float x = 0.0f;
 #pragma unroll 4
@@ -345,9 +347,9 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
         ((T*)io.out)[((size_t)u * G + g) * D + c] = from_f<T>(x);
     }
     Lightest best;
-    const int end = io.positions_out != nullptr || io.weights_out != nullptr ? C : n;
-    for (int j0 = 4 * tid; j0 < end; j0 += kRecords * STEP) {
-        if (j0 > 4 * tid) load_records<NW>(L, u, j0, n, now);
+    const int end = min(j_hi, io.positions_out != nullptr || io.weights_out != nullptr ? C : n);
+    for (int j0 = j_lo + 4 * tid; j0 < end; j0 += kRecords * STEP) {
+        if (j0 > j_lo + 4 * tid) load_records<NW>(L, u, j0, n, now);
 #pragma unroll
         for (int i = 0; i < kRecords; ++i) {
             const int j = j0 + i * STEP;
@@ -388,11 +390,14 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
             }
         }
     }
-    if (n == C) best = lightest_wg<NT>(best, tid);
-    if (tid == 0) {
-        if (io.evicted_out) io.evicted_out[u] = rec.w;
-        write_unit(L, u, n, clock + 1, best);
-    }
+    return n == C ? lightest_wg<NT>(best, tid) : best;
+}
+
+// The record after a step whose lightest token is `best`; one thread.
+__device__ __forceinline__ void step_done(const WeightView& L, const WeightStepIO& io, int u, const int4& rec,
+                                          const Lightest& best) {
+    if (io.evicted_out) io.evicted_out[u] = rec.w;
+    write_unit(L, u, min(rec.x + 1, L.C), rec.y + 1, best);
 }
 
 // ---------------------------------------------------------------------------
@@ -404,7 +409,8 @@ __device__ __forceinline__ void finish_step(const WeightView& L, const WeightSte
 // are on their way or in use.
 // FUSED: one workgroup covers a unit and keeps the logits in LDS. Else one per
 // (unit, split), and the last of a unit's to end finishes the step from what all
-// of them published. STREAM: non-temporal loads.
+// of them published, or (finish_parts) a kernel of several workgroups per unit
+// does. STREAM: non-temporal loads.
 template <typename T, int D, int NW, bool FUSED, bool STREAM>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_weight_step(WeightView L,
                                                                                                  WeightStepIO io) {
@@ -505,7 +511,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     auto o = [&](int i, int g, int c) { return s_o[(size_t)(i * G + g) * (D + 4) + c]; };
     if constexpr (FUSED) {
         auto x4 = [&](int g, int j) { return *reinterpret_cast<const f32x4*>(s_x + (size_t)g * L.cpad + j); };
-        finish_step<T, D, NW>(L, io, u, rec, tid, first, NW, s_w, ml, o, x4);
+        const Lightest best = finish_step<T, D, NW>(L, io, u, rec, tid, 0, L.C, first, NW, s_w, ml, o, x4);
+        if (tid == 0) step_done(L, io, u, rec, best);
     } else {
         float* mlp = L.ml + (size_t)u * nsplit * G * 2;
         float* part = L.part + (size_t)u * nsplit * G * D;
@@ -527,19 +534,57 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 publish(mlp + 2 * (split * G + g) + 1, z);
             }
         }
-        if (!arrive_last(L.arrived + u, nsplit)) return;
+        if (L.finish_parts > 0 || !arrive_last(L.arrived + u, nsplit)) return;
         load_records<NW>(L, u, 4 * tid, n, first);
         auto gml = [&](int i, int g) {
             return make_float2(published(mlp + 2 * (i * G + g)), published(mlp + 2 * (i * G + g) + 1));
         };
         auto go = [&](int i, int g, int c) { return published(part + (size_t)(i * G + g) * D + c); };
         auto x4 = [&](int g, int j) { return published4(xs + (size_t)g * L.cpad + j); };
-        finish_step<T, D, NW>(L, io, u, rec, tid, first, nsplit, s_w, gml, go, x4);
+        const Lightest best = finish_step<T, D, NW>(L, io, u, rec, tid, 0, L.C, first, nsplit, s_w, gml, go, x4);
+        if (tid == 0) step_done(L, io, u, rec, best);
     }
+}
+
+// The end of a step of split units with many tokens: finish_parts workgroups per
+// unit, which take a range of its places each; the last to end picks the
+// lightest token. (One CU reads what the splits left at some 20 GB/s.)
+constexpr int kFinishWaves = 8;
+constexpr int kFinishPlaces = 2048;  // of a workgroup: four a thread
+template <typename T, int D>
+__global__ __launch_bounds__(kFinishWaves * 64) void k_weight_finish(WeightView L, WeightStepIO io) {
+    __shared__ float s_w[(kMaxStepSplits + kMaxPrefixParts) * 16];
+    const int tid = threadIdx.x, parts = L.finish_parts, u = blockIdx.x / parts, part = blockIdx.x - u * parts;
+    if (io.active != nullptr && io.active[u / L.nkv] == 0) return;
+    const int G = L.G, nsplit = L.nsplit, j_lo = part * kFinishPlaces;
+    const int4 rec = *reinterpret_cast<const int4*>(L.unit + (size_t)u * kWeightFields);
+    const float* mlp = L.ml + (size_t)u * nsplit * G * 2;
+    const float* po = L.part + (size_t)u * nsplit * G * D;
+    const float* xs = L.logits + (size_t)u * G * L.cpad;
+    Records first[kRecords];
+    load_records<kFinishWaves>(L, u, j_lo + 4 * tid, min(min(rec.x + 1, L.C), j_lo + kFinishPlaces), first);
+    auto ml = [&](int i, int g) { return *reinterpret_cast<const float2*>(mlp + 2 * (i * G + g)); };
+    auto o = [&](int i, int g, int c) { return po[(size_t)(i * G + g) * D + c]; };
+    auto x4 = [&](int g, int j) { return *reinterpret_cast<const f32x4*>(xs + (size_t)g * L.cpad + j); };
+    const Lightest mine = finish_step<T, D, kFinishWaves>(L, io, u, rec, tid, j_lo, min(L.C, j_lo + kFinishPlaces), first,
+                                                          nsplit, s_w, ml, o, x4);
+    unsigned long long* best = L.best + 2 * ((size_t)u * parts);
+    if (tid == 0) {
+        publish(best + 2 * part, mine.key);
+        publish(best + 2 * part + 1, (unsigned long long)(long long)mine.place);
+    }
+    if (!arrive_last(L.arrived + u, parts)) return;
+    Lightest b;
+    for (int i = tid; i < parts; i += kFinishWaves * 64) b.take(published(best + 2 * i), (int)published(best + 2 * i + 1));
+    b = lightest_wg<kFinishWaves * 64>(b, tid);
+    if (tid == 0) step_done(L, io, u, rec, b);
 }
 
 // Floats of the parts' shares: those of the workgroup's wavefronts or splits, and of the prefix.
 int share_floats(int G, int parts) { return (G * parts + 3) / 4 * 4; }
+
+// A split unit's step ends in a kernel of its own beyond this many bytes.
+constexpr double kFinishBytes = 220e3;
 
 // The fixed part of a step's workgroup in the time of a block, and of a split unit's.
 constexpr int kFusedBlocks = 8, kSplitBlocks = 20;
@@ -554,6 +599,9 @@ hipError_t launch_step_t(const WeightView& L, const WeightStepIO& io, const Weig
                          hipStream_t s) {
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)L.U * p.nsplit), dim3(NW * 64), lds, s, L, io);
+        if (p.finish_parts > 0)
+            hipLaunchKernelGGL((k_weight_finish<T, D>), dim3((unsigned)L.U * p.finish_parts), dim3(kFinishWaves * 64), 0,
+                               s, L, io);
         return hipGetLastError();
     };
     if (stream) return p.fused ? go(k_weight_step<T, D, NW, true, true>) : go(k_weight_step<T, D, NW, false, true>);
@@ -617,6 +665,8 @@ WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16) {
     }
     p.fused = want == 1 && fits(p.waves, 1);
     p.nsplit = want;
+    // (bytes that the end of a unit's step reads and writes)
+    p.finish_parts = !p.fused && (double)C * (4 * G + 20) > kFinishBytes ? (C + kFinishPlaces - 1) / kFinishPlaces : 0;
     return p;
 }
 
@@ -645,6 +695,7 @@ hipError_t launch_weight_step(const WeightView& view, bool bf16, const WeightSte
     WeightView L = view;
     const int parts = (p.fused ? p.waves : p.nsplit) + io.prefix.n;
     L.wfloats = share_floats(L.G, parts);
+    L.finish_parts = p.finish_parts;
     const size_t lds = step_lds(L.G, L.D, L.cpad, p.waves, p.fused, parts);
     auto go = [&](auto w) {
         constexpr int NW = decltype(w)::value;

@@ -102,6 +102,7 @@ struct raas_weight_cache {
     WeightPlan plan;
     void *K = nullptr, *V = nullptr;
     int32_t *pos = nullptr, *unit = nullptr, *arrived = nullptr;
+    unsigned long long* best = nullptr;
     float *w = nullptr, *logits = nullptr, *part = nullptr, *ml = nullptr;
     size_t bytes = 0;
     std::vector<unsigned char> prefilled;
@@ -135,6 +136,7 @@ WeightView view(const raas_weight_cache* c, int layer) {
     L.part = c->part;
     L.ml = c->ml;
     L.arrived = c->arrived;
+    L.best = c->best;
     L.U = c->U;
     L.G = c->G;
     L.D = c->cfg.head_dim;
@@ -253,6 +255,7 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
             {(void**)&c->part, parts * d * 4},
             {(void**)&c->ml, parts * 2 * 4},
             {(void**)&c->arrived, U * 4},
+            {(void**)&c->best, c->plan.finish_parts > 0 ? U * c->plan.finish_parts * 16 : 16},
         };
         const raas_status sa = allocate(reqs, c->bytes, (hipStream_t)stream);
         if (sa != RAAS_OK) {
@@ -273,7 +276,7 @@ void raas_destroy_weight_cache(raas_weight_cache* c) {
     DeviceScope scope(c->device);
     if (c->K) (void)hipStreamSynchronize(c->last_stream);
     for (void* p : {c->K, c->V, (void*)c->pos, (void*)c->w, (void*)c->unit, (void*)c->logits, (void*)c->part,
-                    (void*)c->ml, (void*)c->arrived})
+                    (void*)c->ml, (void*)c->arrived, (void*)c->best})
         if (p) (void)hipFree(p);
     delete c;
 }
