@@ -322,7 +322,7 @@ typedef struct {
 
 typedef struct raas_prefix raas_prefix; /* opaque */
 
-/* Validates cfg, allocates the cache in device memory and clears it on
+/* Validates cfg, allocates the cache in device memory and clears its records on
  * `stream`. The caller releases it with raas_destroy_weight_cache. Errors:
  * RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_HIP. */
 raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream, raas_weight_cache** out);
@@ -406,7 +406,8 @@ raas_status raas_prefix_attention(raas_prefix* prefix, int32_t layer, const void
  * (fp32; entries from lens[b] on are not written). prefix_lse: NULL, or fp32
  * [batch][window][n_q_heads], the log-sum-exp of the same queries over a shared
  * prefix in front of the prompt (raas_prefix_attention), which the softmax
- * then counts. window lies in [1, max(1, max_len)]. workspace: device memory of
+ * then counts. window lies in [1, max(1, max_len)], and window times the
+ * group size is at most 8388608. workspace: device memory of
  * at least raas_prompt_weights_workspace bytes (0 for invalid sizes), which
  * calls that overlap must not share. The tensors lie on the current device.
  * Errors: RAAS_E_INVALID, RAAS_E_HIP. */

@@ -648,7 +648,6 @@ WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16) {
     // more units than CUs: two workgroups of 4 wavefronts per CU, so that one
     // unit's finish overlaps another's reads
     if (U > 256 && fits(4, 2)) p.waves = 4;
-    if (step_lds(G, D, cpad, 8, false, kMaxStepSplits + kMaxPrefixParts) > kStepLds) p.waves = 4;
     // Splits: the number that ends soonest when `per` workgroups run at a time
     // and each takes a fixed part (more of it when the unit is split) besides its
     // blocks, in units of one block at full load.

@@ -18,8 +18,8 @@ namespace {
 
 // Tokens that a unit of a cache, a prefix or a prompt may have.
 constexpr int kMaxTokens = 1 << 20;
-// Query rows of one call over a prefix (the grids' limit).
-constexpr int kMaxQueries = 1 << 17;
+// Query rows of one call over a prefix, and of one KV head's window (the grids' limits).
+constexpr int kMaxQueries = 1 << 17, kMaxWindowRows = 1 << 23;
 
 // The handle's device for the length of a call.
 class DeviceScope {
@@ -60,22 +60,33 @@ raas_status check_heads(int n_q_heads, int n_kv_heads, int head_dim, int dtype) 
     return RAAS_OK;
 }
 
+// A part of a handle's memory; `clear`: it starts at zero.
 struct Req {
     void** ptr;
     size_t bytes;
+    bool clear;
 };
 
-// Allocates and clears (on the stream); the caller frees on failure.
-raas_status allocate(const std::vector<Req>& reqs, size_t& total, hipStream_t s) {
+// One allocation, cut into parts of 256 bytes and up (an allocation takes some
+// 30 us); what must start at zero is cleared on the stream. Keys, values and
+// scratch need not: no place is looked at before it is written, but for the rest
+// of a block, whose logits and values are masked.
+raas_status allocate(const std::vector<Req>& reqs, void** base, size_t& total, hipStream_t s) {
+    auto padded = [](size_t n) { return (n + 255) & ~(size_t)255; };
+    total = 0;
+    for (const Req& r : reqs) total += padded(r.bytes);
+    hipError_t e = hipMalloc(base, total);
+    if (e != hipSuccess) {
+        *base = nullptr;
+        (void)hipGetLastError();
+        return fail(e == hipErrorOutOfMemory ? RAAS_E_OOM : RAAS_E_HIP, "hipMalloc(%zu bytes): %s", total,
+                    hipGetErrorString(e));
+    }
+    char* at = (char*)*base;
     for (const Req& r : reqs) {
-        hipError_t e = hipMalloc(r.ptr, r.bytes);
-        if (e != hipSuccess) {
-            *r.ptr = nullptr;
-            (void)hipGetLastError();
-            return fail(e == hipErrorOutOfMemory ? RAAS_E_OOM : RAAS_E_HIP, "hipMalloc(%zu bytes): %s", r.bytes,
-                        hipGetErrorString(e));
-        }
-        total += r.bytes;
+        *r.ptr = at;
+        at += padded(r.bytes);
+        if (!r.clear) continue;
         e = hipMemsetAsync(*r.ptr, 0, r.bytes, s);
         if (e != hipSuccess) return hip_fail(e, "hipMemsetAsync");
     }
@@ -100,7 +111,7 @@ struct raas_weight_cache {
     int U, G, C, cpad, device;
     bool bf16;
     WeightPlan plan;
-    void *K = nullptr, *V = nullptr;
+    void *memory = nullptr, *K = nullptr, *V = nullptr;
     int32_t *pos = nullptr, *unit = nullptr, *arrived = nullptr;
     unsigned long long* best = nullptr;
     float *w = nullptr, *logits = nullptr, *part = nullptr, *ml = nullptr;
@@ -114,7 +125,7 @@ struct raas_prefix {
     raas_prefix_config cfg;
     int G, tpad, rows, device;
     bool bf16;
-    void *K = nullptr, *V = nullptr;
+    void *memory = nullptr, *K = nullptr, *V = nullptr;
     int32_t* len = nullptr;  // [layers]
     float *part = nullptr, *ml = nullptr;
     size_t bytes = 0;
@@ -165,8 +176,9 @@ raas_status check_layer(const raas_prefix* p, int32_t layer) {
 
 // Whether a step reads its layer of `own` bytes with non-temporal loads, which
 // leave the memory-side cache (256 MB) alone: where too little of the layer is
-// still there (us per step, ordinary / non-temporal, others' bytes in between:
-// NT_FIGURES).
+// still there (us per step, ordinary / non-temporal: 268 MB alone 47.1 / 48.7,
+// in turn with two more caches of that size 58.3 / 52.9; 134 MB 38.0 / 41.8 and
+// 45.8 / 43.4; 67 MB 21.7 / 22.9 and 21.8 / 23.8; 403 MB alone 84.4 / 70.5).
 bool non_temporal(double own, double others) { return others + own * 2.0 / 3.0 > 256e6; }
 
 // The prefix's attention of `rows` sequences' queries into its parts.
@@ -246,18 +258,18 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
         const bool split = !c->plan.fused;
         const size_t parts = split ? U * c->plan.nsplit * c->G : 1;
         const std::vector<Req> reqs = {
-            {&c->K, Ly * U * c->cpad * d * esz},
-            {&c->V, Ly * U * c->cpad * d * esz},
-            {(void**)&c->pos, Ly * U * c->cpad * 4},
-            {(void**)&c->w, Ly * U * c->cpad * 4},
-            {(void**)&c->unit, Ly * U * kWeightFields * 4},
-            {(void**)&c->logits, split ? U * c->G * c->cpad * 4 : 4},
-            {(void**)&c->part, parts * d * 4},
-            {(void**)&c->ml, parts * 2 * 4},
-            {(void**)&c->arrived, U * 4},
-            {(void**)&c->best, c->plan.finish_parts > 0 ? U * c->plan.finish_parts * 16 : 16},
+            {(void**)&c->pos, Ly * U * c->cpad * 4, true},
+            {(void**)&c->w, Ly * U * c->cpad * 4, true},
+            {(void**)&c->unit, Ly * U * kWeightFields * 4, true},
+            {(void**)&c->arrived, U * 4, true},
+            {(void**)&c->best, c->plan.finish_parts > 0 ? U * c->plan.finish_parts * 16 : 16, false},
+            {(void**)&c->logits, split ? U * c->G * c->cpad * 4 : 4, false},
+            {(void**)&c->part, parts * d * 4, false},
+            {(void**)&c->ml, parts * 2 * 4, false},
+            {&c->K, Ly * U * c->cpad * d * esz, false},
+            {&c->V, Ly * U * c->cpad * d * esz, false},
         };
-        const raas_status sa = allocate(reqs, c->bytes, (hipStream_t)stream);
+        const raas_status sa = allocate(reqs, &c->memory, c->bytes, (hipStream_t)stream);
         if (sa != RAAS_OK) {
             raas_destroy_weight_cache(c);
             return sa;
@@ -274,10 +286,10 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
 void raas_destroy_weight_cache(raas_weight_cache* c) {
     if (!c) return;
     DeviceScope scope(c->device);
-    if (c->K) (void)hipStreamSynchronize(c->last_stream);
-    for (void* p : {c->K, c->V, (void*)c->pos, (void*)c->w, (void*)c->unit, (void*)c->logits, (void*)c->part,
-                    (void*)c->ml, (void*)c->arrived, (void*)c->best})
-        if (p) (void)hipFree(p);
+    if (c->memory) {
+        (void)hipStreamSynchronize(c->last_stream);
+        (void)hipFree(c->memory);
+    }
     delete c;
 }
 
@@ -427,13 +439,13 @@ raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas
         const size_t Ly = (size_t)cfg->n_layers, d = (size_t)cfg->head_dim, esz = p->bf16 ? 2 : 4;
         const size_t parts = prefix_scratch_rows(cfg->n_kv_heads, cfg->max_rows * p->G);
         const std::vector<Req> reqs = {
-            {&p->K, Ly * cfg->n_kv_heads * p->tpad * d * esz},
-            {&p->V, Ly * cfg->n_kv_heads * p->tpad * d * esz},
-            {(void**)&p->len, Ly * 4},
-            {(void**)&p->part, parts * d * 4},
-            {(void**)&p->ml, parts * 2 * 4},
+            {(void**)&p->len, Ly * 4, true},
+            {(void**)&p->part, parts * d * 4, false},
+            {(void**)&p->ml, parts * 2 * 4, false},
+            {&p->K, Ly * cfg->n_kv_heads * p->tpad * d * esz, false},
+            {&p->V, Ly * cfg->n_kv_heads * p->tpad * d * esz, false},
         };
-        const raas_status sa = allocate(reqs, p->bytes, (hipStream_t)stream);
+        const raas_status sa = allocate(reqs, &p->memory, p->bytes, (hipStream_t)stream);
         if (sa != RAAS_OK) {
             raas_destroy_prefix(p);
             return sa;
@@ -450,9 +462,10 @@ raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas
 void raas_destroy_prefix(raas_prefix* p) {
     if (!p) return;
     DeviceScope scope(p->device);
-    if (p->K) (void)hipStreamSynchronize(p->last_stream);
-    for (void* q : {p->K, p->V, (void*)p->len, (void*)p->part, (void*)p->ml})
-        if (q) (void)hipFree(q);
+    if (p->memory) {
+        (void)hipStreamSynchronize(p->last_stream);
+        (void)hipFree(p->memory);
+    }
     delete p;
 }
 
@@ -520,6 +533,8 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
         return fail(RAAS_E_INVALID, "max_len must lie in [0, %d] (got %d)", kMaxTokens, max_len);
     if (window < 1 || window > std::max(1, max_len))
         return fail(RAAS_E_INVALID, "window must lie in [1, max_len = %d] (got %d)", max_len, window);
+    if ((long long)window * (n_q_heads / n_kv_heads) > kMaxWindowRows)
+        return fail(RAAS_E_INVALID, "window * n_q_heads / n_kv_heads must be at most %d", kMaxWindowRows);
     for (int b = 0; b < batch && lens; ++b)
         if (lens[b] < 0 || lens[b] > max_len)
             return fail(RAAS_E_INVALID, "lens[%d] = %d outside [0, max_len = %d]", b, lens[b], max_len);

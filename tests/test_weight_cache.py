@@ -148,6 +148,7 @@ STEPS = [
     (5, 14, 2, 64, 50, 8, "f32", [50, 1, 0, 33, 50], 12, 130, 0),
     (1, 4, 1, 128, 1100, 64, "bf16", [1100], 8, 1, 0),
     (9, 32, 4, 128, 64, 8, "bf16", [64] * 9, 8, 500, 0),
+    (100, 32, 2, 64, 2048, 100, "bf16", [60 - i % 9 for i in range(100)], 3, 0, 0),  # logits that do not fit LDS
     (1, 4, 1, 64, 9000, 3000, "f32", [8995], 12, 0, 0),   # the end of a step in a kernel of its own
     (2, 16, 1, 128, 4100, 100, "bf16", [4100, 50], 6, 40, 1),
 ]

@@ -80,7 +80,8 @@ CACHE = HEADS + [dict(batch=0), dict(capacity=1), dict(capacity=(1 << 20) + 1), 
 PREFIX = HEADS + [dict(max_tokens=0), dict(max_tokens=(1 << 20) + 1), dict(max_rows=0), dict(max_rows=1 << 22)]
 PROMPT = HEADS[:-1] + [dict(batch=0), dict(max_len=-1), dict(max_len=(1 << 20) + 1), dict(window=0), dict(window=65),
                        dict(lens=(64, 65)), dict(lens=(-1, 3)), dict(q=None), dict(k=None), dict(weights=None),
-                       dict(workspace=None), dict(space=1)]
+                       dict(workspace=None), dict(space=1),
+                       dict(n_q_heads=32, max_len=1 << 20, window=1 << 20)]
 _ids = lambda bad: ",".join("%s=%s" % kv for kv in bad.items())  # noqa: E731
 
 
