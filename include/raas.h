@@ -293,12 +293,14 @@ raas_status raas_profile_read(raas_pool* pool, int32_t kernel, double* total_ms,
  *      summed over the G heads (fp32; the new token's start at 0).
  * The conventions above hold: device tensors (aligned to their element type),
  * head-major layouts, nothing awaited (but by the export and the destroys),
- * finite inputs, calls on one handle ordered. Outputs are bitwise
- * reproducible. Steps, prefix attention and prompt weights allocate nothing
- * and copy nothing from the host, so they may be captured into a HIP graph,
- * and a replay works on what the cache and the prefix hold then; graphs of one
- * handle are ordered like its calls (they share its scratch). A handle's calls
- * run on the device that was current at its creation. */
+ * finite inputs, calls on one handle ordered. The same calls on the same state
+ * give the same bits. Steps, prefix attention and prompt weights allocate
+ * nothing and copy nothing from the host, so they may be captured into a HIP
+ * graph, and a replay works on what the cache and the prefix hold then (cutting
+ * the prefix into the parts of the length at capture, which rounds otherwise
+ * than another length's); graphs of one handle are ordered like its calls (they
+ * share its scratch). A handle's calls run on the device that was current at its
+ * creation. */
 typedef struct {
     int32_t batch;      /* sequences, >= 1; batch * n_kv_heads <= 1000000 */
     int32_t n_layers;   /* >= 1 */

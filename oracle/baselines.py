@@ -1,6 +1,7 @@
 """Retention policies to set beside page-level RaaS -- TEST INFRASTRUCTURE ONLY.
 
-Oracle-only references (no GPU code implements them): plain fp64 numpy
+References only (of these the library runs H2O's policy on the GPU, as the
+weight cache, which evicts when the next token arrives): plain fp64 numpy
 statements of the policies the paper compares with (Section 4: dense
 attention, StreamingLLM's sink-plus-window, H2O's heavy hitters, Quest's
 query-aware page selection) and of token-level RaaS (Section 3.2, the policy

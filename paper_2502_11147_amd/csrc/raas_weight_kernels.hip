@@ -308,7 +308,7 @@ __device__ __forceinline__ void load_records(const WeightView& L, int u, int j, 
 // 746, the records' reads too 729).
 template <typename T, int D, int NW, bool STREAM, class Ml, class O, class X4>
 __device__ __forceinline__ Lightest finish_step(const WeightView& L, const WeightStepIO& io, int u, const int4& rec,
-                                            int tid, int j_lo, int j_hi, Records (&now)[kRecords], int nsrc,
+                                                int tid, int j_lo, int j_hi, Records (&now)[kRecords], int nsrc,
                                                 float* s_w, Ml ml, O o, X4 x4) {
     constexpr int NT = NW * 64, STEP = NT * 4;
     __shared__ float s_m[16], s_rz[16];
@@ -594,10 +594,17 @@ __global__ __launch_bounds__(kFinishWaves * 64) void k_weight_finish(WeightView 
 // Floats of the parts' shares: those of the workgroup's wavefronts or splits, and of the prefix.
 int share_floats(int G, int parts) { return (G * parts + 3) / 4 * 4; }
 
-// A split unit's step ends in a kernel of its own beyond this many bytes.
+// A split unit's step ends in a kernel of its own beyond this many bytes (us, in
+// the step kernel / of its own, 8 KV heads of G = 4: 2 sequences of 6000 tokens
+// 22.4 / 22.5, 4 of 8201 44.4 / 42.4, 1 of 16384 34.8 / 27.5; 4 of 3000 20.0 /
+// 22.2).
 constexpr double kFinishBytes = 220e3;
 
-// The fixed part of a step's workgroup in the time of a block, and of a split unit's.
+// The fixed part of a step's workgroup in the time of a block, and of a split
+// unit's (us with kSplitBlocks 10 / 20, 8 KV heads: 20 sequences of 2048 tokens
+// 50.8 / 37.3, 24 of 4096 100.5 / 73.5; the one-unit fp32 cache of 256 tokens 9.9
+// / 8.7; with 512 workgroups wanted whatever the rounds, 8 of 2048 28.2 against
+// 21.7 and 16 of 4096 74.9 against 62.2).
 constexpr int kFusedBlocks = 8, kSplitBlocks = 20;
 
 size_t step_lds(int G, int D, int cpad, int nw, bool fused, int parts) {
@@ -657,7 +664,9 @@ WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16) {
     };
     p.waves = 8;
     // more units than CUs: two workgroups of 4 wavefronts per CU, so that one
-    // unit's finish overlaps another's reads
+    // unit's finish overlaps another's reads (us, 8 / 4 wavefronts, 8 KV heads: 40
+    // sequences of 3000 tokens 118.4 / 104.6, 64 of 1024 57.2 / 52.6, 100 of 512
+    // 64.8 / 52.0, 128 of 2048 199.5 / 197.5)
     if (U > 256 && fits(4, 2)) p.waves = 4;
     // Splits: the number that ends soonest when `per` workgroups run at a time
     // and each takes a fixed part (more of it when the unit is split) besides its

@@ -479,6 +479,69 @@ def test_side_stream():
         assert torch.equal(a, b)
 
 
+def test_two_streams_at_once():
+    """Two caches with a prefix each, stepped on two streams with nothing between
+    them, as each alone: the same bits."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case weight two streams")
+    rng = np.random.default_rng(6)
+    B, Hq, Hkv, d, C = 5, 8, 2, 128, 3000
+    mk = lambda *shape: _data(rng, shape, "bf16")[0]  # noqa: E731
+    data = [[mk(Hkv, 400, d), mk(Hkv, 400, d), mk(B, Hkv, C, d), mk(B, Hkv, C, d), mk(9, B, Hq, d), mk(9, B, Hkv, d),
+             mk(9, B, Hkv, d)] for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for together in (False, True):
+        torch.cuda.synchronize()
+        made = []
+        for (sk, sv, k0, v0, _, _, _), s in zip(data, streams):
+            p = raas.SharedPrefix(1, Hq, Hkv, d, 400, B, stream=s)
+            c = raas.WeightCache(B, 1, Hq, Hkv, d, C, 100, stream=s)
+            p.store(0, sk, sv, stream=s)
+            c.prefill(0, k0, v0, stream=s)
+            made.append((c, p, torch.zeros(9, B, Hq, d, dtype=torch.bfloat16, device="cuda"),
+                         torch.zeros(B, Hkv, C, device="cuda")))
+        torch.cuda.synchronize()
+        order = [(i, t) for t in range(9) for i in range(2)] if together else [(i, t) for i in range(2) for t in range(9)]
+        for i, t in order:
+            c, p, out, w = made[i]
+            c.decode_step(0, data[i][4][t], data[i][5][t], data[i][6][t], out[t], weights=w, prefix=p, stream=streams[i])
+            if not together:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        got.append([x for m in made for x in m[2:]])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_load_kinds_round_alike():
+    """A layer that other caches' steps push out of the memory-side cache is read
+    with other loads: the same bits."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case weight load kinds")
+    B, Hq, Hkv, d, C = 32, 16, 8, 128, 2048
+    g = torch.Generator(device="cuda").manual_seed(3)
+    mk = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()  # noqa: E731
+    k0, v0, q, k, v = mk(B, Hkv, C, d), mk(B, Hkv, C, d), mk(6, B, Hq, d), mk(6, B, Hkv, d), mk(6, B, Hkv, d)
+    caches = [raas.WeightCache(B, 1, Hq, Hkv, d, C, 100) for _ in range(3)]
+    for c in caches:
+        c.prefill(0, k0, v0)
+    outs = [(torch.zeros_like(q), torch.zeros(B, Hkv, C, device="cuda")) for _ in range(2)]
+    for t in range(6):  # alone
+        caches[0].decode_step(0, q[t], k[t], v[t], outs[0][0][t], weights=outs[0][1])
+    for t in range(6):  # with another one's steps in between
+        caches[1].decode_step(0, q[t], k[t], v[t], outs[1][0][t], weights=outs[1][1])
+        caches[2].decode_step(0, q[t], k[t], v[t], torch.empty_like(q[t]))
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
 def test_offsets_past_two_to_the_31():
     """The last unit's rows lie past 2^31 elements in both handles."""
     import torch
