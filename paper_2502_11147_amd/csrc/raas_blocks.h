@@ -179,8 +179,8 @@ __device__ __forceinline__ void load_row(const T* row, bool real, int a, u32x4 (
 }
 
 // VE probabilities as the operand that multiplies values: rounded to bf16 beside
-// bf16 values (the matrix cores take no other type there; the errors, half a step
-// of 2^-8 each, average out over the tokens and stay below the output's own
+// bf16 values (the matrix cores take no other type there; the errors, at most
+// 2^-8 of each, average out over the tokens and stay below the output's own
 // rounding).
 template <typename T>
 __device__ __forceinline__ u32x4 pack(const float (&p)[kVec<T>]) {
@@ -213,10 +213,8 @@ struct Softmax {
 
 // One block of `valid` (1 .. tokens of a block) tokens against a tile of 16
 // queries: x[q][r] receives the logits (base 2) of token VE a + 4 q + r, -inf
-// from `valid` on. Sums are kept in fp32; the probabilities that multiply bf16
-// values are rounded to bf16 (the matrix cores take no other type beside them;
-// their errors, 2^-9 each, average out over the tokens and stay below the
-// output's own rounding), the sum of the probabilities takes them unrounded.
+// from `valid` on. Sums are kept in fp32; the sum of the probabilities takes them
+// as they are before pack.
 template <typename T, int D>
 __device__ __forceinline__ void attend(const u32x4 (&kr)[D / 16], const u32x4 (&vr)[D / 16],
                                        const u32x4 (&q)[D / (4 * kVec<T>)], int valid, int a, float scale_log2,

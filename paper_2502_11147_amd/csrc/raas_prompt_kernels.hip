@@ -345,8 +345,8 @@ void launch_t(const PromptView& v, const SeqLens& lens, int most, hipStream_t s)
 
 // Workgroups wanted in each of the two kernels: about six per CU, so that the
 // causal part's uneven ones even out (a prompt of 4096 tokens, every query: 214 us
-// with 700, 197 with 1536, 204 with 3072, each of which starts with its rows or
-// keys once more).
+// with 700, 197 with 1536, 204 with twice as many, each of which starts with its
+// rows or keys once more).
 constexpr int kWorkgroups = 1536;
 
 }  // namespace
