@@ -120,21 +120,22 @@ __device__ __forceinline__ uint32_t dpp(uint32_t x) {
 }
 template <int CTRL>
 __device__ __forceinline__ float dpp_f(float x) { return __uint_as_float(dpp<CTRL>(__float_as_uint(x))); }
-// max and sum over a wavefront, the same on each lane
-__device__ __forceinline__ float wave_max(float x) {
+// max and sum over lanes 16 a .. 16 a + 15, the same on each
+__device__ __forceinline__ float row16_max(float x) {
     x = fmaxf(x, dpp_f<0xB1>(x));
     x = fmaxf(x, dpp_f<0x4E>(x));
     x = fmaxf(x, dpp_f<0x141>(x));
-    x = fmaxf(x, dpp_f<0x140>(x));
-    return max_groups(x);
+    return fmaxf(x, dpp_f<0x140>(x));
 }
-__device__ __forceinline__ float wave_sum(float x) {
+__device__ __forceinline__ float row16_sum(float x) {
     x += dpp_f<0xB1>(x);
     x += dpp_f<0x4E>(x);
     x += dpp_f<0x141>(x);
-    x += dpp_f<0x140>(x);
-    return sum_groups(x);
+    return x + dpp_f<0x140>(x);
 }
+// and over a wavefront
+__device__ __forceinline__ float wave_max(float x) { return max_groups(row16_max(x)); }
+__device__ __forceinline__ float wave_sum(float x) { return sum_groups(row16_sum(x)); }
 // min of 64-bit values over a wavefront, the same on each lane
 __device__ __forceinline__ unsigned long long wave_min(unsigned long long x) {
     auto with = [&](uint32_t lo, uint32_t hi) {

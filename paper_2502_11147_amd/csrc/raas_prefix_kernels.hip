@@ -271,36 +271,45 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     }
 }
 
-// Output and log-sum-exp of every row from the parts: one wavefront per row, a
-// lane per part for the maximum and the sum (kMaxPrefixParts is 64). The KV head
-// comes first in the grid here as in the kernels above, so that with eight of
-// them the parts are read on the XCD that wrote them (1024 rows in 16 parts: 9.2
-// -> 5.0 us). Over an empty prefix the output is 0 and the log-sum-exp -inf.
-template <typename T, int D>
+// Output and log-sum-exp of every row from at most PARTS parts: one wavefront per
+// row, a lane per part for the maximum and the sum, then 16 bytes per lane of 4
+// (D 64) or 2 parts at a time. All of a row's reads are on their way together
+// (60 rows in 64 parts, D 64: 17.3 -> 3.1 us). The KV head comes first in the
+// grid here as in the kernels above, so that with eight of them the parts are
+// read on the XCD that wrote them (1024 rows in 16 parts: 9.2 -> 5.0 us). Over an
+// empty prefix the output is 0 and the log-sum-exp -inf.
+template <typename T, int D, int PARTS>
 __global__ __launch_bounds__(256) void k_prefix_join(PrefixView P, T* __restrict__ out, float* __restrict__ lse) {
+    constexpr int LANES = D / 4, AT = 64 / LANES, READS = PARTS / AT;  // lanes of a row, parts at a time
+    typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     const int h = blockIdx.x, r = blockIdx.y * 4 + wave_of(threadIdx.x), lane = threadIdx.x & 63;
     if (r >= P.rows) return;
     const size_t rows = (size_t)P.nkv * P.rows, i = (size_t)h * P.rows + r;
-    const int seq = r / P.G;
+    const int seq = r / P.G, c = lane % LANES * 4;
     const size_t to = (size_t)seq * P.nkv * P.G + h * P.G + (r - seq * P.G);
-    static_assert(kMaxPrefixParts <= 64, "");
+    f32x4 y[READS];
+#pragma unroll
+    for (int s = 0; s < READS; ++s)  // (past the last part: that one again, which weighs 0 there)
+        y[s] = *reinterpret_cast<const f32x4*>(P.part + (min(s * AT + lane / LANES, P.nsplit - 1) * rows + i) * D + c);
     float2 ml = make_float2(-INFINITY, 0.0f);
     if (lane < P.nsplit) ml = *reinterpret_cast<const float2*>(P.ml + 2 * (lane * rows + i));
-    float M = ml.x, x[D / 64] = {};
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+    const float M = wave_max(ml.x);
     const float e = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - M);
-    float Z = ml.y * e;
+    const float Z = wave_sum(ml.y * e);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) Z += __shfl_xor(Z, d);
-#pragma unroll 8
-    for (int s = 0; s < P.nsplit; ++s) {
-        const float es = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e), s));
+    for (int s = 0; s < READS; ++s) x += y[s] * __shfl(e, s * AT + lane / LANES);
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) x[c] += P.part[(s * rows + i) * D + 64 * c + lane] * es;
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (AT == 4) x[k] = sum_groups(x[k]);
+        else x[k] += __shfl_xor(x[k], 32);
     }
+    if (lane < LANES) {
+        T4 o;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) out[to * D + 64 * c + lane] = from_f<T>(Z > 0.0f ? x[c] / Z : 0.0f);
+        for (int k = 0; k < 4; ++k) o[k] = from_f<T>(Z > 0.0f ? x[k] / Z : 0.0f);
+        *reinterpret_cast<T4*>(out + to * D + c) = o;
+    }
     if (lse != nullptr && lane == 0)
         lse[to] = Z > 0.0f ? (M + __builtin_amdgcn_logf(Z)) * 0.69314718055994530942f : -INFINITY;
 }
@@ -309,7 +318,10 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixView P, T* __restrict
 // prefix once per 32 rows but needs no step of all wavefronts per block (us, few
 // / many: 48 rows of 8 KV heads, 32768 tokens 34.2 / 43.1, 64 rows, 4096 tokens
 // 15.4 / 14.1, 128 rows 24.9 / 22.7, 128 rows and 32768 tokens 92.5 / 48.8).
-int wide(int rows) { return rows > 128 ? 8 : rows > 64 ? 4 : 0; }
+// Four where eight would leave half a tile empty (us, 8 / 4 wavefronts: 368 rows
+// of 4 KV heads, 8520 tokens, fp32 87.0 / 72.7, bf16 25.5 / 26.1, 896 rows of 2
+// with a step 61.0 / 56.9).
+int wide(int rows) { return rows <= 64 ? 0 : (rows + 127) / 128 % 2 == 1 ? 4 : 8; }
 // rows of a workgroup's tile, and the tiles
 int row_tile(int rows) { return wide(rows) ? wide(rows) * 16 * kWideTiles : rows <= 16 ? 16 : 32; }
 int row_tiles(int rows) { return (rows + row_tile(rows) - 1) / row_tile(rows); }
@@ -327,8 +339,14 @@ void launch_t(const PrefixView& P, const void* q, hipStream_t s) {
 
 template <typename T, int D>
 void join_t(const PrefixView& P, void* out, float* lse, hipStream_t s) {
-    hipLaunchKernelGGL((k_prefix_join<T, D>), dim3(P.nkv, (P.rows + 3) / 4), dim3(256), 0, s, P, (T*)out,
-                       lse);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(P.nkv, (P.rows + 3) / 4), dim3(256), 0, s, P, (T*)out, lse);
+    };
+    static_assert(kMaxPrefixParts <= 64, "");
+    if (P.nsplit <= 8) go(k_prefix_join<T, D, 8>);
+    else if (P.nsplit <= 16) go(k_prefix_join<T, D, 16>);
+    else if (P.nsplit <= 32) go(k_prefix_join<T, D, 32>);
+    else go(k_prefix_join<T, D, 64>);
 }
 
 // workgroups that fill the chip
@@ -343,8 +361,10 @@ int plan_prefix(int nkv, int rows, int tokens, bool bf16) {
     // and joining it (us with 1 / 2 / 4 per wavefront: 32 rows, 8192 tokens 23.1 /
     // 19.9 / 20.3, 16 rows, 4096 tokens 11.8 / 11.6 / 12.9; with 4 / 8 / 16 blocks:
     // 128 rows, 4096 tokens 30.3 / 22.7 / 22.4, 160 rows, 700 tokens 15.2 / 17.6 /
-    // 19.2)
-    const int least = wide(rows) ? 8 : 2 * kWaves;
+    // 19.2). An fp32 block is half the tokens at eight times the work: fewer (us, 2
+    // / 1 per wavefront: 40 rows, 2000 tokens 25.9 / 23.4; 8 / 2 blocks: 124 rows,
+    // 270 tokens 22.6 / 14.7).
+    const int least = wide(rows) ? (bf16 ? 8 : 2) : bf16 ? 2 * kWaves : kWaves;
     return std::max(1, std::min(want, (nb + least - 1) / least));
 }
 
@@ -354,7 +374,9 @@ size_t prefix_scratch_rows(int nkv, int rows) {
         const int x = nkv * row_tiles(r);
         return (size_t)std::min(std::max(workgroups(r), x), kMaxPrefixParts * x) * row_tile(r);
     };
-    return std::max({most(std::min(rows, 16)), most(std::min(rows, 32)), most(std::min(rows, 128)), most(rows)});
+    // (the most rows of either width, and of the few-rows kernels)
+    return std::max({most(std::min(rows, 16)), most(std::min(rows, 64)), most(std::min(rows, 128)),
+                     most(rows > 128 ? (rows - 1) / 128 * 128 : rows), most(rows)});
 }
 
 hipError_t launch_prefix_attention(const PrefixView& P, bool bf16, const void* q, hipStream_t s) {

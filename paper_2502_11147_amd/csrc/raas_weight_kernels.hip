@@ -301,6 +301,19 @@ __device__ __forceinline__ void load_records(const WeightView& L, int u, int j, 
     for (int i = 0; i < kRecords; ++i) now[i].load<STREAM>(L, u, j + i * NW * 256, n);
 }
 
+// x += the first n parts' values by their shares, N of them on their way together
+// (past the last part: that one again, without weight).
+template <int N, class Value, class Share>
+__device__ __forceinline__ void add_parts(float& x, int n, Value value, Share share) {
+    for (int s0 = 0; s0 < n; s0 += N) {
+        float y[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) y[k] = value(min(s0 + k, n - 1));
+#pragma unroll
+        for (int k = 0; k < N; ++k) x = __builtin_fmaf(y[k], s0 + k < n ? share(s0 + k) : 0.0f, x);
+    }
+}
+
 // The outputs are written past the caches, and the records read and written so
 // where the layer does not stay in them (STREAM): as lines leave an L2 by
 // themselves, writes come between the other units' reads (128 sequences of 8 KV
@@ -348,10 +361,10 @@ __device__ __forceinline__ Lightest finish_step(const WeightView& L, const Weigh
     for (int i = tid; i < (j_lo == 0 ? G * D : 0); i += NT) {
         const int g = i / D, c = i % D;
         float x = 0.0f;
-#pragma unroll 4
-        for (int s = 0; s < nsrc; ++s) x += o(s, g, c) * s_w[s * G + g];
-#pragma unroll 4
-        for (int s = 0; s < pp.n; ++s) x += pp.o[(s * rows + row0 + g) * D + c] * s_w[(nsrc + s) * G + g];
+        add_parts<8>(x, nsrc, [&](int s) { return o(s, g, c); }, [&](int s) { return s_w[s * G + g]; });
+        add_parts<8>(
+            x, pp.n, [&](int s) { return pp.o[(s * rows + row0 + g) * D + c]; },
+            [&](int s) { return s_w[(nsrc + s) * G + g]; });
         ((T*)io.out)[((size_t)u * G + g) * D + c] = from_f<T>(x);
     }
     Lightest best;

@@ -248,9 +248,18 @@ def prompt_weights(q, k, weights, lens=None, prefix_lse=None, stream=None):
     wp = _pointer(weights, "weights", torch.float32, (B, Hkv, P), dev)
     lp = _pointer(prefix_lse, "prefix_lse", torch.float32, (B, W, Hq), dev, optional=True)
     need = int(lib.raas_prompt_weights_workspace(B, Hq, Hkv, P, W))
-    stream = torch.cuda.current_stream(dev) if stream is None else stream
-    with torch.cuda.device(dev), torch.cuda.stream(stream):
+    current = torch.cuda.current_stream(dev)
+    if stream is None:
+        stream = current
+
+    def call():
         space = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
         _check(lib.raas_prompt_weights(B, Hq, Hkv, d, code, qp, kp, lp, _host_ints(lens, B, "lens"), P, W, wp,
                                        space.data_ptr(), need, stream.cuda_stream),
                "raas_prompt_weights")
+
+    if dev == torch.cuda.current_device() and stream == current:
+        call()
+    else:  # (the workspace belongs to the stream that uses it)
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            call()
