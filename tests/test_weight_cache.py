@@ -272,6 +272,36 @@ def test_prefix_attention(case):
     p.close()
 
 
+@pytest.mark.parametrize("dtype,Hkv,n", [("bf16", 1, 2100), ("bf16", 3, 1500), ("f32", 2, 1100)])
+def test_prefix_rows_of_one_handle(dtype, Hkv, n):
+    """Fewer rows than the handle may take: every tile of rows and number of parts
+    fits its scratch."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case prefix rows %s %d" % (dtype, Hkv))
+    G, d, most = 2, 64, 330
+    rng = np.random.default_rng(n)
+    p = raas.SharedPrefix(1, G * Hkv, Hkv, d, n, most, dtype)
+    (k, K), (v, V) = (_data(rng, (Hkv, n, d), dtype) for _ in range(2))
+    p.store(0, k, v)
+    q, Q = _data(rng, (most, G * Hkv, d), dtype)
+    want = []
+    for h in range(Hkv):
+        x = Q[:, h * G:(h + 1) * G].reshape(-1, d)
+        o, bound, lse, lb = ref.prefix_attention(x, K[h], V[h], dtype == "bf16")
+        want.append([y.reshape((most, G) + y.shape[1:]) for y in (o, bound, lse, lb)])
+    o, bound, lse, lb = (np.concatenate(x, axis=1) for x in zip(*want))
+    for rows in (1, 8, 9, 16, 17, 32, 33, 64, 65, 128, 129, 192, 193, 256, 257, 320, 321, 330):
+        out = torch.full((rows, G * Hkv, d), 9.0, dtype=q.dtype, device="cuda")
+        got = torch.full((rows, G * Hkv), 9.0, device="cuda")
+        p.attend(0, q[:rows], out, got)
+        _within(_np(out), o[:rows], bound[:rows], rows)
+        _within(_np(got), lse[:rows], lb[:rows], rows)
+    p.close()
+
+
 def test_empty_prefix():
     import torch
 
@@ -298,6 +328,8 @@ PROMPT = [
     ([300], 4, 1, 128, 300, "bf16", 0), ([700, 255, 64], 8, 4, 64, 20, "bf16", 0), ([130, 129], 16, 1, 128, 130, "f32", 0),
     ([2100, 900], 4, 2, 128, 3, "bf16", 0), ([1111], 14, 2, 64, 1, "f32", 0), ([40, 2, 600], 3, 1, 64, 64, "bf16", 0),
     ([9] * 300, 1, 1, 64, 4, "f32", 0),
+    # (more than 16 pieces of the keys, and of the rows)
+    ([9001, 5, 4500], 2, 1, 64, 3, "bf16", 0), ([1200, 70], 4, 1, 64, 1200, "bf16", 0), ([5003], 6, 2, 128, 2, "f32", 0),
 ]
 
 
