@@ -357,15 +357,24 @@ int workgroups(int rows) { return wide(rows) == 4 ? 512 : 256; }
 int plan_prefix(int nkv, int rows, int tokens, bool bf16) {
     const int bt = bf16 ? 32 : 16, nb = (tokens + bt - 1) / bt;
     const int want = std::min(kMaxPrefixParts, std::max(1, workgroups(rows) / (nkv * row_tiles(rows))));
-    // blocks of a part: two per wavefront, or (many rows) enough to pay for writing
-    // and joining it (us with 1 / 2 / 4 per wavefront: 32 rows, 8192 tokens 23.1 /
-    // 19.9 / 20.3, 16 rows, 4096 tokens 11.8 / 11.6 / 12.9; with 4 / 8 / 16 blocks:
-    // 128 rows, 4096 tokens 30.3 / 22.7 / 22.4, 160 rows, 700 tokens 15.2 / 17.6 /
-    // 19.2). An fp32 block is half the tokens at eight times the work: fewer (us, 2
-    // / 1 per wavefront: 40 rows, 2000 tokens 25.9 / 23.4; 8 / 2 blocks: 124 rows,
-    // 270 tokens 22.6 / 14.7).
-    const int least = wide(rows) ? (bf16 ? 8 : 2) : bf16 ? 2 * kWaves : kWaves;
-    return std::max(1, std::min(want, (nb + least - 1) / least));
+    int parts;
+    if (wide(rows)) {
+        // A part takes the time of its blocks, one after the other, and writing and
+        // joining its rows takes that of a bf16 block per 4096 rows of all heads:
+        // the least of nb / parts + parts * rows / 4096 (us with parts of 8 / 4 blocks
+        // / by this rule, 8 KV heads of G = 4: 40 sequences over 700 tokens 15.8 / 13.1
+        // / 12.6, 64 over 1024 18.2 / 16.1 / 16.2, 32 over 8192 18.4 / 24.0 / 18.6; an
+        // fp32 block is half the tokens at eight times the work: 124 rows, 270 tokens
+        // 14.4, with parts of 8 blocks 22.6).
+        parts = (int)lround(sqrt((double)nb * (bf16 ? 4096 : 16384) / ((double)nkv * rows)));
+    } else {
+        // two blocks per wavefront (us with 1 / 2 / 4: 32 rows, 8192 tokens 23.1 / 19.9
+        // / 20.3, 16 rows, 4096 tokens 11.8 / 11.6 / 12.9); of fp32, half the tokens at
+        // eight times the work, one (40 rows, 2000 tokens: 23.4, with two 25.9)
+        const int least = bf16 ? 2 * kWaves : kWaves;
+        parts = (nb + least - 1) / least;
+    }
+    return std::max(1, std::min({want, parts, nb}));
 }
 
 size_t prefix_scratch_rows(int nkv, int rows) {
