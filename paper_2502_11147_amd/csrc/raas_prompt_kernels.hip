@@ -369,10 +369,12 @@ PromptPlan plan_prompt(int units, int G, int W, int P, bool bf16) {
     const long long rows = (long long)W * G;
     // at least 256 keys or rows a piece (us with 512 / 256 / 128, 8 KV heads: 1 prompt
     // of 2000 tokens, window 64 31.6 / 24.9 / 28.1, 4 of 300, every query 33.9 / 26.5 /
-    // 29.8, 1 of 16000, window 32 29.2 / 30.4 / 31.0)
+    // 29.8, 1 of 16000, window 32 29.2 / 30.4 / 31.0); of fp32, whose products take
+    // eight times as long, 64 (with 256 / 128 / 64: 1 of 957, window 35 47.2 / 38.4 /
+    // 32.3, 1 of 500, every query 69.8 / 64.7 / 54.1)
     auto pieces = [&](long long n, long long others, long long tile, int& count, int& size) {
         const long long wgs = units * ((others + tile - 1) / tile);
-        const long long want = std::max(1LL, std::min<long long>(kWorkgroups / wgs, n / 256));
+        const long long want = std::max(1LL, std::min<long long>(kWorkgroups / wgs, n / (bf16 ? 256 : 64)));
         size = (int)(((n + want - 1) / want + kStage - 1) / kStage * kStage);
         count = (int)((n + size - 1) / size);
     };
