@@ -179,24 +179,32 @@ __device__ __forceinline__ void load_row(const T* row, bool real, int a, u32x4 (
         q[ks] = real ? ld16_in<T>(row + 4 * kVec<T> * ks + kVec<T> * a) : u32x4{0u, 0u, 0u, 0u};
 }
 
-// VE probabilities as the operand that multiplies values: rounded to bf16 beside
-// bf16 values (the matrix cores take no other type there; the errors, at most
-// 2^-8 of each, average out over the tokens and stay below the output's own
-// rounding).
+// VE probabilities as the operand that multiplies values. Beside bf16 values the
+// matrix cores take bf16 only, so each is the sum of two there: its upper 16 bits
+// and what they leave, rounded to bf16, which is off by at most 2^-15 of it. (One
+// bf16 alone is off by 2^-8: where values of either sign cancel, its errors do so
+// no better than the values, and the outputs were off by 0.0020 to 0.0025 of their
+// size where their own rounding is 0.0017. The second product is free where
+// reading bounds a kernel, the step and the prefix of few rows; k_prefix_wide has
+// what it costs there.)
 template <typename T>
-__device__ __forceinline__ u32x4 pack(const float (&p)[kVec<T>]) {
-    u32x4 v;
-    if constexpr (sizeof(T) == 2) {
-        bf16x8 b;
+struct Probs {
+    u32x4 hi, lo;  // (lo: bf16 only)
+    __device__ __forceinline__ explicit Probs(const float (&p)[kVec<T>]) {
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 rest;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) b[j] = (__bf16)p[j];
-        v = __builtin_bit_cast(u32x4, b);
-    } else {
+            for (int j = 0; j < 8; ++j) rest[j] = (__bf16)(p[j] - __uint_as_float(__float_as_uint(p[j]) & 0xFFFF0000u));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(p[j]);
+            for (int j = 0; j < 4; ++j)
+                hi[j] = __float_as_uint(p[2 * j]) >> 16 | (__float_as_uint(p[2 * j + 1]) & 0xFFFF0000u);
+            lo = __builtin_bit_cast(u32x4, rest);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) hi[j] = __float_as_uint(p[j]);
+        }
     }
-    return v;
-}
+};
 
 // Running softmax of one query column: maximum (base 2), this lane's share of
 // the sum, and the accumulated values' rows 16 ct + 4 a + r.
@@ -214,8 +222,7 @@ struct Softmax {
 
 // One block of `valid` (1 .. tokens of a block) tokens against a tile of 16
 // queries: x[q][r] receives the logits (base 2) of token VE a + 4 q + r, -inf
-// from `valid` on. Sums are kept in fp32; the sum of the probabilities takes them
-// as they are before pack.
+// from `valid` on. Sums are kept in fp32.
 template <typename T, int D>
 __device__ __forceinline__ void attend(const u32x4 (&kr)[D / 16], const u32x4 (&vr)[D / 16],
                                        const u32x4 (&q)[D / (4 * kVec<T>)], int valid, int a, float scale_log2,
@@ -252,9 +259,12 @@ __device__ __forceinline__ void attend(const u32x4 (&kr)[D / 16], const u32x4 (&
             p[4 * t + r] = __builtin_amdgcn_exp2f(x[t][r] - s.m);
             s.l += p[4 * t + r];
         }
-    const u32x4 pv = pack<T>(p);
+    const Probs<T> pv(p);
 #pragma unroll
-    for (int ct = 0; ct < D / 16; ++ct) s.o[ct] = mfma16<T>(vr[ct], pv, s.o[ct]);
+    for (int ct = 0; ct < D / 16; ++ct) s.o[ct] = mfma16<T>(vr[ct], pv.hi, s.o[ct]);
+    if constexpr (sizeof(T) == 2)
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct) s.o[ct] = mfma16<T>(vr[ct], pv.lo, s.o[ct]);
 }
 
 // Order-preserving unsigned key of a float (NaN above +inf).

@@ -111,8 +111,11 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
 // wavefronts hold 32 rows each and share the blocks of the part through LDS,
 // where one lies ready while two more are on their way in registers; blocks are
 // stored in operand order, so both sides of LDS are consecutive. Bound by the
-// matrix cores and the exponentials: 32 products of 16 cycles a block and
-// wavefront beside about as many cycles of vector work. A wavefront has both in
+// matrix cores and the exponentials: 48 products (bf16, head_dim 128) of 16 cycles
+// a block and wavefront beside about as many cycles of vector work. 16 of the
+// products are those of the probabilities' lower halves (us without / with them,
+// 8 KV heads of G = 4: 128 sequences over 32768 tokens 81 / 102, 64 over 8192 26.9
+// / 30.4, 32 over 4096 15.2 / 16.2). A wavefront has both in
 // flight, as the logits of the next block are formed while this one's
 // probabilities are; so a block's keys are staged with the values of the one
 // before. Eight wavefronts where there are the rows: two per SIMD in step with
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
             }
         }
         logits(buf, xn);  // (past the part's end: the last block's again, unused)
-        u32x4 pv[RT];
+        u32x4 ph[RT], pl[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             float p[VE], l = 0.0f;
@@ -227,13 +230,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
                     l += p[4 * c + e];
                 }
             s[t].l += l;
-            pv[t] = pack<T>(p);
+            const Probs<T> pv(p);
+            ph[t] = pv.hi;
+            if constexpr (sizeof(T) == 2) pl[t] = pv.lo;
         }
 #pragma unroll
         for (int ct = 0; ct < NP; ++ct) {
             const u32x4 v = s_kv[buf][(NP + ct) * 64 + lane];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) s[t].o[ct] = mfma16<T>(v, pv[t], s[t].o[ct]);
+            for (int t = 0; t < RT; ++t) s[t].o[ct] = mfma16<T>(v, ph[t], s[t].o[ct]);
+            if constexpr (sizeof(T) == 2)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) s[t].o[ct] = mfma16<T>(v, pl[t], s[t].o[ct]);
         }
         store(buf ^ 1, next);
         load(b + 4, next);

@@ -1,0 +1,108 @@
+"""How exact the weight cache's step, the shared prefix and the prompt weights
+are, on the GPU against 64 bits: bf16 probabilities' halves, logits far from 0.
+
+Bounds. With u = 2^-24 the softmax and the sums are off by rel A, as
+tests/weight_reference.py derives it (A = sum_j a_j |v_j|). Beside bf16 values a
+probability is the sum of its upper 16 bits, which leave less than 2^-7 of it,
+and of that rest rounded to bf16 (half a step, 2^-8): off by 2^-15 of itself, and
+an output by 2^-15 A. What is then rounded to bf16 moves by 2^-8 of its size."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import weight_reference as ref
+from harness import say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2502_11147_amd as raas
+
+    raas.load_library()
+
+
+def _data(rng, shape):
+    import torch
+
+    x = torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).bfloat16()
+    return x.cuda(), x.double().numpy()
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _attention(q, K, V):
+    """(out, its bound) of q [rows][d] over K, V [n][d], bf16."""
+    x, dx = ref.logits(q, K)
+    a = np.exp(x - x.max(axis=1, keepdims=True))
+    a /= a.sum(axis=1, keepdims=True)
+    out, A = a @ V, a @ np.abs(V)
+    bound = ref.softmax_error(dx, x)[:, None] * A + 2.0 ** -15 * A + 2 * ref.U32 * np.abs(out)
+    return out, bound + 2.0 ** -8 * (np.abs(out) + bound) + 1e-37
+
+
+def _within(got, want, bound, what):
+    over = np.abs(got - want) - bound
+    at = np.unravel_index(np.argmax(over), over.shape)
+    assert over[at] <= 0, (what, at, got[at], want[at], bound[at])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [3, 20, 65, 129])  # of G = 2: every prefix kernel
+def test_prefix_probabilities(rows, d):
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case precision prefix %d %d" % (rows, d))
+    Hq, Hkv, n = 4, 2, 700
+    rng = np.random.default_rng(rows)
+    (k, K), (v, V), (q, Q) = _data(rng, (Hkv, n, d)), _data(rng, (Hkv, n, d)), _data(rng, (rows, Hq, d))
+    p = raas.SharedPrefix(1, Hq, Hkv, d, n, rows, "bf16")
+    p.store(0, k, v)
+    out = torch.empty_like(q)
+    p.attend(0, q, out)
+    for h in range(Hkv):
+        want, bound = _attention(Q[:, 2 * h:2 * h + 2].reshape(-1, d), K[h], V[h])
+        _within(_np(out)[:, 2 * h:2 * h + 2].reshape(-1, d), want, bound, h)
+    p.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("batch,capacity,prefix", [(2, 200, 0), (1, 3000, 0), (3, 100, 300), (140, 90, 0)])
+def test_step_probabilities(batch, capacity, prefix, d):
+    """One workgroup per unit, several, a prefix besides, workgroups of four wavefronts."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case precision step %d %d %d %d" % (batch, capacity, prefix, d))
+    Hq, Hkv, n = 8, 2, capacity - 1
+    rng = np.random.default_rng(capacity)
+    (k, K), (v, V) = _data(rng, (batch, Hkv, n, d)), _data(rng, (batch, Hkv, n, d))
+    (q, Q), (kn, KN), (vn, VN) = _data(rng, (batch, Hq, d)), _data(rng, (batch, Hkv, d)), _data(rng, (batch, Hkv, d))
+    c = raas.WeightCache(batch, 1, Hq, Hkv, d, capacity, 10, "bf16")
+    c.prefill(0, k, v)
+    p = PK = PV = None
+    if prefix:
+        (pk, PK), (pv, PV) = _data(rng, (Hkv, prefix, d)), _data(rng, (Hkv, prefix, d))
+        p = raas.SharedPrefix(1, Hq, Hkv, d, prefix, batch, "bf16")
+        p.store(0, pk, pv)
+    out = torch.empty_like(q)
+    c.decode_step(0, q, kn, vn, out, prefix=p)
+    G = Hq // Hkv
+    for b in range(batch):
+        for h in range(Hkv):
+            keys, values = [K[b, h], KN[b, h][None]], [V[b, h], VN[b, h][None]]
+            if prefix:
+                keys, values = keys + [PK[h]], values + [PV[h]]
+            want, bound = _attention(Q[b, h * G:(h + 1) * G], np.concatenate(keys), np.concatenate(values))
+            _within(_np(out)[b, h * G:(h + 1) * G], want, bound, (b, h))
+    c.close()
