@@ -220,6 +220,20 @@ PromptSpace prompt_space(int batch, int n_q_heads, int n_kv_heads, int max_len, 
     return sp;
 }
 
+// The sizes that a call of the prompt weights may have.
+raas_status check_prompt(int batch, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int max_len, int window) {
+    if (batch < 1) return fail(RAAS_E_INVALID, "batch must be >= 1 (got %d)", batch);
+    const raas_status st = check_heads(n_q_heads, n_kv_heads, head_dim, dtype);
+    if (st != RAAS_OK) return st;
+    if (max_len < 0 || max_len > kMaxTokens)
+        return fail(RAAS_E_INVALID, "max_len must lie in [0, %d] (got %d)", kMaxTokens, max_len);
+    if (window < 1 || window > std::max(1, max_len))
+        return fail(RAAS_E_INVALID, "window must lie in [1, max_len = %d] (got %d)", max_len, window);
+    if ((long long)window * (n_q_heads / n_kv_heads) > kMaxWindowRows)
+        return fail(RAAS_E_INVALID, "window * n_q_heads / n_kv_heads must be at most %d", kMaxWindowRows);
+    return RAAS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -511,9 +525,7 @@ raas_status raas_prefix_attention(raas_prefix* p, int32_t layer, const void* q, 
 
 size_t raas_prompt_weights_workspace(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len,
                                      int32_t window) {
-    if (batch < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads != 0 || max_len < 1 ||
-        window < 1)
-        return 0;
+    if (check_prompt(batch, n_q_heads, n_kv_heads, 64, RAAS_F32, max_len, window) != RAAS_OK || max_len == 0) return 0;
     size_t most = 0;  // over both types, which are cut differently
     for (bool bf16 : {false, true}) {
         const PromptSpace sp = prompt_space(batch, n_q_heads, n_kv_heads, max_len, window, bf16);
@@ -526,15 +538,8 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
                                 const void* q, const void* k, const float* prefix_lse, const int32_t* lens,
                                 int32_t max_len, int32_t window, float* weights, void* workspace,
                                 size_t workspace_bytes, void* stream) {
-    if (batch < 1) return fail(RAAS_E_INVALID, "batch must be >= 1 (got %d)", batch);
-    const raas_status st = check_heads(n_q_heads, n_kv_heads, head_dim, dtype);
+    const raas_status st = check_prompt(batch, n_q_heads, n_kv_heads, head_dim, dtype, max_len, window);
     if (st != RAAS_OK) return st;
-    if (max_len < 0 || max_len > kMaxTokens)
-        return fail(RAAS_E_INVALID, "max_len must lie in [0, %d] (got %d)", kMaxTokens, max_len);
-    if (window < 1 || window > std::max(1, max_len))
-        return fail(RAAS_E_INVALID, "window must lie in [1, max_len = %d] (got %d)", max_len, window);
-    if ((long long)window * (n_q_heads / n_kv_heads) > kMaxWindowRows)
-        return fail(RAAS_E_INVALID, "window * n_q_heads / n_kv_heads must be at most %d", kMaxWindowRows);
     for (int b = 0; b < batch && lens; ++b)
         if (lens[b] < 0 || lens[b] > max_len)
             return fail(RAAS_E_INVALID, "lens[%d] = %d outside [0, max_len = %d]", b, lens[b], max_len);

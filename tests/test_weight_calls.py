@@ -1,0 +1,41 @@
+"""Calls around the weight cache that other tests leave out: sizes that a query
+must refuse, workspaces of any float alignment."""
+from __future__ import annotations
+
+import os
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2502_11147_amd as raas
+
+    if not os.path.exists(raas.LIB_PATH):
+        from paper_2502_11147_amd import build as b
+
+        b.build()
+    return raas.load_library()
+
+
+# batch, query heads, KV heads, max_len, window
+REFUSED = [(0, 8, 2, 64, 64), (1, 7, 2, 64, 64), (1, 0, 1, 64, 64), (1, 1, 0, 64, 64), (1, 34, 2, 64, 64),
+           (1, 65536, 65536, 64, 64), (1, 8, 2, -1, 1), (1, 8, 2, (1 << 20) + 1, 64), (1, 8, 2, 2 ** 31 - 1, 64),
+           (1, 8, 2, 64, 0), (1, 8, 2, 64, 65), (1, 8, 2, 64, 2 ** 31 - 1), (1, 16, 1, 1 << 20, 1 << 20)]
+
+
+@pytest.mark.parametrize("sizes", REFUSED)
+def test_workspace_of_refused_sizes_is_zero(lib, sizes):
+    """The query and the call refuse the same sizes (the pointers are not followed)."""
+    import paper_2502_11147_amd as raas
+
+    assert lib.raas_prompt_weights_workspace(*sizes) == 0
+    batch, hq, hkv, max_len, window = sizes
+    assert lib.raas_prompt_weights(batch, hq, hkv, 64, raas.F32, 64, 64, None, None, max_len, window, 64, 64, 1 << 40,
+                                   None) == raas.E_INVALID
+
+
+@pytest.mark.parametrize("sizes", [(1, 1, 1, 1, 1), (3, 14, 2, 700, 9), (1, 16, 1, 1 << 20, 1 << 19), (1, 65535, 65535, 8, 8)])
+def test_workspace_of_allowed_sizes(lib, sizes):
+    assert lib.raas_prompt_weights_workspace(*sizes) > 0
+    assert lib.raas_prompt_weights_workspace(*sizes[:3], 0, 1) == 0  # nothing to do
