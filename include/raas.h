@@ -411,7 +411,8 @@ raas_status raas_prefix_attention(raas_prefix* prefix, int32_t layer, const void
  * then counts. window lies in [1, max(1, max_len)], and window times the
  * group size is at most 8388608. workspace: device memory of
  * at least raas_prompt_weights_workspace bytes (0 for sizes that the call
- * refuses, and for max_len 0), which calls that overlap must not share. The tensors lie on the current device.
+ * refuses, and for max_len 0), aligned to 4 bytes, which calls that overlap must
+ * not share. The tensors lie on the current device.
  * Errors: RAAS_E_INVALID, RAAS_E_HIP. */
 size_t raas_prompt_weights_workspace(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len,
                                      int32_t window);

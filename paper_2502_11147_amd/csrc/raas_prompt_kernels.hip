@@ -74,6 +74,9 @@ struct Staged {
     }
 };
 
+// Two floats of the workspace, which is aligned to one.
+typedef float f32x2_in __attribute__((ext_vector_type(2), aligned(4)));
+
 // The log-sum-exp (base 2) of row r of a unit, from its maximum and sum over
 // the prompt's keys; the prefix's joins them.
 __device__ __forceinline__ float row_lse(const PromptView& v, int b, int h, int r, float M, float Z) {
@@ -110,9 +113,9 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(PromptView v, SeqLens 
     const int chunks = (len - nq + query_of(v, r)) / v.chunk_keys + 1;  // those that hold keys for it
     float M = kNothing, Z = 0.0f;
     for (int c = lane; c < chunks; c += 16) {
-        const float2 x = *reinterpret_cast<const float2*>(ml + 2 * c);
-        const float m = fmaxf(M, x.x);
-        Z = Z * __builtin_amdgcn_exp2f(M - m) + x.y * __builtin_amdgcn_exp2f(x.x - m);
+        const f32x2_in x = *reinterpret_cast<const f32x2_in*>(ml + 2 * c);
+        const float m = fmaxf(M, x[0]);
+        Z = Z * __builtin_amdgcn_exp2f(M - m) + x[1] * __builtin_amdgcn_exp2f(x[0] - m);
         M = m;
     }
     const float most = row16_max(M);

@@ -39,3 +39,30 @@ def test_workspace_of_refused_sizes_is_zero(lib, sizes):
 def test_workspace_of_allowed_sizes(lib, sizes):
     assert lib.raas_prompt_weights_workspace(*sizes) > 0
     assert lib.raas_prompt_weights_workspace(*sizes[:3], 0, 1) == 0  # nothing to do
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shift", [1, 2, 3])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_workspace_of_any_float_alignment(dtype, shift):
+    """Seven heads and a window of one: the pairs of a row's maximum and sum
+    start at an odd float; so do they behind a shifted workspace. The same bits."""
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2502_11147_amd as raas
+
+    lib = raas.load_library()
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(shift)
+    P = 2100  # several pieces of the keys
+    q, k = (torch.randn(*s, generator=g, device="cuda").to(dt) for s in ((1, 1, 7, 64), (1, 7, P, 64)))
+    want, got = torch.zeros(1, 7, P, device="cuda"), torch.zeros(1, 7, P, device="cuda")
+    raas.prompt_weights(q, k, want)
+    need = lib.raas_prompt_weights_workspace(1, 7, 7, P, 1)
+    space = torch.full((need // 4 + shift,), float("nan"), device="cuda")
+    rc = lib.raas_prompt_weights(1, 7, 7, 64, raas.BF16 if dtype == "bf16" else raas.F32, q.data_ptr(), k.data_ptr(), None,
+                                 None, P, 1, got.data_ptr(), space[shift:].data_ptr(), need,
+                                 torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == 0 and torch.equal(want, got) and abs(float(got.sum()) - 7.0) < 1e-3
