@@ -1,10 +1,10 @@
 // gfx950 kernels of the prompt weights: what the queries of a prompt's last
 // `window` tokens give each of its tokens,
-//   x_ij = q_i . k_j / sqrt(d), j <= i;  lse_i = log sum_j exp(x_ij)
-//   w_j = sum_{i >= j} exp(x_ij - lse_i), over the group's heads besides.
-// A first kernel finds each query row's maximum and sum, a second one walks
-// the rows that see a tile of keys and adds their probabilities up in
-// registers: the products are computed twice, but no probability is written
+//   x_ij = q_i . k_j / sqrt(d), j <= i;  m_i = max_j x_ij
+//   w_j = sum_{i >= j} exp(x_ij - m_i) / sum_j' exp(x_ij' - m_i), over the
+// group's heads besides. A first kernel finds each query row's maximum and sum,
+// a second one walks the rows that see a tile of keys and adds their
+// probabilities up in registers: the products are computed twice, but no probability is written
 // (a window of the whole prompt has as many as P^2 / 2 per head), and no
 // atomic changes the order of a sum.
 #include <math.h>
@@ -74,32 +74,34 @@ struct Staged {
     }
 };
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 // Two floats of the workspace, which is aligned to one.
 typedef float f32x2_in __attribute__((ext_vector_type(2), aligned(4)));
 
-// The log-sum-exp (base 2) of row r of a unit, from its maximum and sum over
-// the prompt's keys; the prefix's joins them.
-__device__ __forceinline__ float row_lse(const PromptView& v, int b, int h, int r, float M, float Z) {
+// What the second kernel needs of row r of a unit, from its maximum and sum over
+// the prompt's keys: the maximum and the sum's inverse, those over a prefix
+// counted in. They stay apart: a log-sum-exp would round at its own size, which
+// far from 0 is much more than a probability's. (The maximum's own rounding cancels
+// between numerator and sum.)
+__device__ __forceinline__ f32x2_in row_stat(const PromptView& v, int b, int h, int r, float M, float Z) {
     if (v.prefix_lse != nullptr) {
+        constexpr float kLog2e = 1.44269504088896340736f, kRest = (float)(1.44269504088896340736 - (double)kLog2e);
         const int i = query_of(v, r);
-        const float pre = v.prefix_lse[((size_t)b * v.W + i) * v.nkv * v.G + (size_t)h * v.G + (r - i * v.G)] *
-                          1.44269504088896340736f;
-        const float m = fmaxf(M, pre);
-        Z = Z * __builtin_amdgcn_exp2f(M - m) + __builtin_amdgcn_exp2f(pre - m);
+        const float lse = v.prefix_lse[((size_t)b * v.W + i) * v.nkv * v.G + (size_t)h * v.G + (r - i * v.G)];
+        const float pre = lse * kLog2e, m = fmaxf(M, pre);
+        // (what the product's rounding left; of an empty prefix, -inf, nothing)
+        const float rest = pre == -INFINITY ? 0.0f : __builtin_fmaf(lse, kRest, __builtin_fmaf(lse, kLog2e, -pre));
+        Z = Z * __builtin_amdgcn_exp2f(M - m) + __builtin_amdgcn_exp2f(pre - m + rest);
         M = m;
     }
-    return M + __builtin_amdgcn_logf(Z);
+    return f32x2_in{M, 1.0f / Z};
 }
-// A row's maximum and sum over one chunk: its log-sum-exp if there is no other.
+// A row's maximum and sum over one chunk: what the second kernel needs if there is no other.
 __device__ __forceinline__ void row_done(const PromptView& v, int unit, int b, int h, int r, int chunk, float M,
                                          float Z) {
     const size_t at = (size_t)unit * v.W * v.G + r;
-    if (v.chunks == 1) {
-        v.lse[at] = row_lse(v, b, h, r, M, Z);
-    } else {
-        v.ml[2 * (at * v.chunks + chunk)] = M;
-        v.ml[2 * (at * v.chunks + chunk) + 1] = Z;
-    }
+    if (v.chunks == 1) *reinterpret_cast<f32x2_in*>(v.stat + 2 * at) = row_stat(v, b, h, r, M, Z);
+    else *reinterpret_cast<f32x2_in*>(v.ml + 2 * (at * v.chunks + chunk)) = f32x2_in{M, Z};
 }
 
 // The chunks of a row joined, 16 lanes a row. Grid: rows, units.
@@ -121,7 +123,8 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(PromptView v, SeqLens 
     const float most = row16_max(M);
     Z = row16_sum(Z * __builtin_amdgcn_exp2f(M - most));
     if (lane == 0 && row < nq * v.G)
-        v.lse[(size_t)unit * v.W * v.G + r] = row_lse(v, v.seq0 + unit / v.nkv, unit % v.nkv, r, most, Z);
+        *reinterpret_cast<f32x2_in*>(v.stat + 2 * ((size_t)unit * v.W * v.G + r)) =
+            row_stat(v, v.seq0 + unit / v.nkv, unit % v.nkv, r, most, Z);
 }
 
 // Maximum (base 2) and sum of every query row over a chunk of keys. Grid:
@@ -241,15 +244,17 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
 
 // Probabilities of a chunk of query rows, summed per key. Grid: units, key
 // tiles (the ones that most rows see first), row chunks. A wavefront holds kHeld
-// tiles of 16 keys; the rows pass through LDS with their log-sum-exp (base 2).
-// Bound as the kernel above.
+// tiles of 16 keys; the rows pass through LDS with their maximum (base 2) and the
+// inverse of their sum.
+// Bound as the kernel above. Three wavefronts per SIMD at head_dim 64, where two
+// registers too many would leave two (a whole prompt of 3000 tokens 94.6 us, 97).
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_keys(PromptView v,
-                                                                                                   SeqLens lens) {
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void k_prompt_keys(
+    PromptView v, SeqLens lens) {
     constexpr int KS = D / (4 * kVec<T>), KT = kHeld<T>, SUB = kStage / 16, HALVES = Staged<T, D>::HALVES;
     constexpr int WG_KEYS = kWaves * 16 * KT;
     __shared__ __align__(16) u32x4 s_q[HALVES][kStage * D / kVec<T>];
-    __shared__ float s_lse[HALVES][kStage];
+    __shared__ f32x2 s_stat[HALVES][kStage];
     const int tid = threadIdx.x, lane = tid & 63, w = wave_of(tid), a = lane >> 4, col = lane & 15;
     const int unit = blockIdx.x, b = v.seq0 + unit / v.nkv, h = unit % v.nkv;
     const int len = lens.len[unit / v.nkv], nq = seq_rows(v, len), rows = nq * v.G;
@@ -267,18 +272,20 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
     const int first = max(0, wg0 - (len - nq)) * v.G, mine = max(0, j0 - (len - nq)) * v.G;
     const int lo = blockIdx.z * v.chunk_rows, hi = min(rows, lo + v.chunk_rows);
     Staged<T, D> next;
-    float lse = 0.0f;
+    f32x2 stat = {0.f, 0.f};
     auto load = [&](int r0) {
         next.load(tid, [&](int r) { return query_row<T, D>(v, b, h, min(r0 + r, rows - 1)); });
         if (tid >= kStage) return;
         // (rows behind the last weigh nothing)
-        lse = r0 + tid < rows ? v.lse[(size_t)unit * v.W * v.G + r0 + tid] : INFINITY;
+        stat = f32x2{INFINITY, 0.f};
+        if (r0 + tid < rows)
+            stat = *reinterpret_cast<const f32x2_in*>(v.stat + 2 * ((size_t)unit * v.W * v.G + r0 + tid));
     };
     const int start = max(lo, first) / kStage * kStage;
     if (start < hi) load(start);
     for (int r0 = start, buf = 0; r0 < hi; r0 += kStage, buf = (buf + 1) % HALVES) {
         next.store(tid, s_q[buf]);
-        if (tid < kStage) s_lse[buf][tid] = lse;
+        if (tid < kStage) s_stat[buf][tid] = stat;
         lds_barrier();
         if (r0 + kStage < hi) load(r0 + kStage);
         if (r0 + kStage <= mine || j0 >= len) continue;
@@ -288,7 +295,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
             for (int c = 0; c < SUB; ++c) {
                 u32x4 q[KS];
                 Staged<T, D>::read(s_q[buf], c, a, col, q);
-                const float off = s_lse[buf][16 * c + col];
+                const f32x2 st = s_stat[buf][16 * c + col];
                 const int last = masked ? len - nq + query_of(v, r0 + 16 * c + col) : 0;
                 f32x4 x[KT];
 #pragma unroll
@@ -301,9 +308,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
                 for (int t = 0; t < KT; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float y = __builtin_fmaf(x[t][e], v.scale_log2, -off);
-                        sum[t][e] +=
-                            __builtin_amdgcn_exp2f(masked && j0 + 16 * t + 4 * a + e > last ? -INFINITY : y);
+                        const float y = __builtin_fmaf(x[t][e], v.scale_log2, -st[0]);
+                        const float p = __builtin_amdgcn_exp2f(masked && j0 + 16 * t + 4 * a + e > last ? -INFINITY : y);
+                        sum[t][e] = __builtin_fmaf(p, st[1], sum[t][e]);
                     }
             }
         };

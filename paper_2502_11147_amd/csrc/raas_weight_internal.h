@@ -118,7 +118,7 @@ struct PromptView : PromptPlan {
     const void* k;           // [B][nkv][P][D]
     const float* prefix_lse; // [B][W][Hq] or NULL
     float* weights;          // [B][nkv][P]
-    float* lse;              // [nseq * nkv][W * G] scratch: each row's log-sum-exp (base 2)
+    float* stat;             // [nseq * nkv][W * G][2] scratch: each row's maximum (base 2) and 1 / sum
     float* ml;               // [nseq * nkv][W * G][chunks][2] scratch, if chunks > 1: maxima and sums
     float* part;             // [row_chunks][nseq * nkv][P] scratch, if row_chunks > 1
     int W, P, G, D, nkv, seq0, nseq;

@@ -207,15 +207,15 @@ raas_status prefix_parts(raas_prefix* p, int32_t layer, const void* q, int rows,
 struct PromptSpace {
     int nseq;
     PromptPlan plan;
-    size_t lse, ml, part;
+    size_t stat, ml, part;
 };
 PromptSpace prompt_space(int batch, int n_q_heads, int n_kv_heads, int max_len, int window, bool bf16) {
     PromptSpace sp;
     sp.nseq = std::min({batch, kLenSeqs, std::max(1, 65535 / n_kv_heads)});
     const int W = std::min(window, max_len);
     sp.plan = plan_prompt(sp.nseq * n_kv_heads, n_q_heads / n_kv_heads, W, max_len, bf16);
-    sp.lse = (size_t)sp.nseq * n_q_heads * W;
-    sp.ml = sp.plan.chunks > 1 ? sp.lse * sp.plan.chunks * 2 : 0;
+    sp.stat = (size_t)sp.nseq * n_q_heads * W * 2;
+    sp.ml = sp.plan.chunks > 1 ? sp.stat * sp.plan.chunks : 0;
     sp.part = sp.plan.row_chunks > 1 ? (size_t)sp.plan.row_chunks * sp.nseq * n_kv_heads * max_len : 0;
     return sp;
 }
@@ -529,7 +529,7 @@ size_t raas_prompt_weights_workspace(int32_t batch, int32_t n_q_heads, int32_t n
     size_t most = 0;  // over both types, which are cut differently
     for (bool bf16 : {false, true}) {
         const PromptSpace sp = prompt_space(batch, n_q_heads, n_kv_heads, max_len, window, bf16);
-        most = std::max(most, sp.lse + sp.ml + sp.part);
+        most = std::max(most, sp.stat + sp.ml + sp.part);
     }
     return most * sizeof(float);
 }
@@ -555,8 +555,8 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
     v.k = k;
     v.prefix_lse = prefix_lse;
     v.weights = weights;
-    v.lse = (float*)workspace;
-    v.ml = v.lse + sp.lse;
+    v.stat = (float*)workspace;
+    v.ml = v.stat + sp.stat;
     v.part = v.ml + sp.ml;
     v.W = window;
     v.P = max_len;

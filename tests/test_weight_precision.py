@@ -106,3 +106,63 @@ def test_step_probabilities(batch, capacity, prefix, d):
             want, bound = _attention(Q[b, h * G:(h + 1) * G], np.concatenate(keys), np.concatenate(values))
             _within(_np(out)[b, h * G:(h + 1) * G], want, bound, (b, h))
     c.close()
+
+
+def _prompt(Q, K, lse):
+    """(weights, relative error allowed) of one unit: Q [rows][G][d], K [n][d], lse [rows][G] or None.
+
+    For inputs whose products are exact, so that a logit is rounded only at the
+    distance from its row's maximum, Y at most (base 2): a probability is off by
+    ln 2 * 2 u Y for that, as much for the factor log2(e) / sqrt(d), a few u for
+    exponentials and the inverse, n u for the sum it is divided by, doubled where
+    numerator and sum have it both; then rows * G of them are added.
+    With a prefix that factor's rounding no longer cancels: the logits are off by
+    a common delta x, |delta| <= u, and the prefix's sum is not, so that of p_j =
+    exp(x_j (1 + delta)) / (sum exp(x (1 + delta)) + exp(lse)) the logarithm moves
+    by delta (x_j - sum_j a_j x_j), with sum_j a_j <= 1: by u max |x| at most,
+    as any logit held in fp32 does."""
+    rows, G, d = Q.shape
+    n = len(K)
+    w, Y, X = np.zeros(n), 0.0, 0.0
+    for i in range(rows):
+        last = n - rows + i + 1
+        x = Q[i] @ K[:last].T / np.sqrt(d)
+        m = x.max(axis=1)
+        if lse is not None:
+            m = np.maximum(m, lse[i])
+        e = np.exp(x - m[:, None])
+        z = e.sum(axis=1)
+        if lse is not None:
+            z = z + np.exp(lse[i] - m)
+            X = max(X, np.abs(x).max())
+        w[:last] += (e / z[:, None]).sum(axis=0)
+        Y = max(Y, (m[:, None] - x).max() / np.log(2.0))
+    return w, (4 * np.log(2.0) * Y + n + rows * G + 32 + X) * ref.U32
+
+
+@pytest.mark.parametrize("prefixed", [False, True])
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,n,W", [("f32", 2, 2, 64, 60, 1), ("bf16", 2, 1, 64, 90, 5), ("bf16", 6, 2, 128, 100, 1),
+                                                ("f32", 4, 2, 128, 200, 3), ("bf16", 4, 4, 128, 150, 150), ("bf16", 2, 1, 64, 600, 2)])
+def test_prompt_weights_of_far_logits(dtype, Hq, Hkv, d, n, W, prefixed):
+    """Logits some 2000 or 2900 from 0 and a few apart (integers, so that products are exact)."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case precision prompt %s %d %d %d %s" % (dtype, d, n, W, prefixed))
+    rng = np.random.default_rng(n + W)
+    Q = 16.0 + rng.integers(-1, 2, (1, W, Hq, d))
+    K = 16.0 + rng.integers(-1, 2, (1, Hkv, n, d))
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q, k = (torch.from_numpy(x).to(dt).cuda() for x in (Q, K))
+    lse = lse64 = None
+    if prefixed:
+        lse = (256.0 * np.sqrt(d) + 10.0 + 3.0 * rng.standard_normal((1, W, Hq))).astype(np.float32)
+        lse64, lse = lse.astype(np.float64), torch.from_numpy(lse).cuda()
+    w = torch.zeros(1, Hkv, n, device="cuda")
+    raas.prompt_weights(q, k, w, prefix_lse=lse)
+    G = Hq // Hkv
+    for h in range(Hkv):
+        heads = slice(h * G, (h + 1) * G)
+        want, rel = _prompt(Q[0, :, heads], K[0, h], None if lse64 is None else lse64[0, :, heads])
+        _within(_np(w)[0, h], want, rel * want + 1e-37, h)
