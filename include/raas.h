@@ -293,7 +293,9 @@ raas_status raas_profile_read(raas_pool* pool, int32_t kernel, double* total_ms,
  *      summed over the G heads (fp32; the new token's start at 0).
  * The conventions above hold: device tensors (aligned to their element type),
  * head-major layouts, nothing awaited (but by the export and the destroys),
- * finite inputs, calls on one handle ordered. The same calls on the same state
+ * finite inputs (whose scaled logits lie within 5e8 of 0: further out the
+ * rounding of a logit alone passes the range of an exponential), calls on one
+ * handle ordered. The same calls on the same state
  * give the same bits. Steps, prefix attention and prompt weights allocate
  * nothing and copy nothing from the host, so they may be captured into a HIP
  * graph, and a replay works on what the cache and the prefix hold then (cutting

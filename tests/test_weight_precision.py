@@ -166,3 +166,52 @@ def test_prompt_weights_of_far_logits(dtype, Hq, Hkv, d, n, W, prefixed):
         heads = slice(h * G, (h + 1) * G)
         want, rel = _prompt(Q[0, :, heads], K[0, h], None if lse64 is None else lse64[0, :, heads])
         _within(_np(w)[0, h], want, rel * want + 1e-37, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_equal_logits_at_the_limit(sign, dtype):
+    """Logits of +-4e8, all equal (their products are exact): even weights, the values' mean.
+
+    n + 64 roundings of the sums, and of the mean's type; a log-sum-exp moves by
+    a few roundings at its size."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    say("case precision limit %s %g" % (dtype, sign))
+    rng = np.random.default_rng(5)
+    Hq, Hkv, d, n = 4, 2, 64, 300
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    const = lambda c, *shape: torch.full(shape, c, dtype=dt, device="cuda")  # noqa: E731
+    x = sign * 8192.0 * 6144.0 * d / np.sqrt(d)
+    v = torch.from_numpy(rng.standard_normal((Hkv, n, d)).astype(np.float32)).to(dt).cuda()
+    V = _np(v)
+
+    def mean(got, V, what):
+        want, A = V.mean(axis=0), np.abs(V).mean(axis=0)
+        bound = (len(V) + 64) * ref.U32 * A
+        if dtype == "bf16":
+            bound = bound + 2.0 ** -15 * A
+            bound = bound + 2.0 ** -8 * (np.abs(want) + bound)
+        _within(got, np.broadcast_to(want, got.shape), bound, what)
+
+    p = raas.SharedPrefix(1, Hq, Hkv, d, n, 140, dtype)
+    p.store(0, const(sign * 6144.0, Hkv, n, d), v)
+    for rows in (3, 12, 40, 70, 140):
+        out, lse = const(9.0, rows, Hq, d), torch.zeros(rows, Hq, device="cuda")
+        p.attend(0, const(8192.0, rows, Hq, d), out, lse)
+        for h in range(Hkv):
+            mean(_np(out)[:, 2 * h:2 * h + 2].reshape(-1, d), V[h], (rows, h))
+        assert np.abs(_np(lse) - x).max() <= 8 * ref.U32 * abs(x)
+    w = torch.zeros(1, Hkv, n, device="cuda")
+    raas.prompt_weights(const(8192.0, 1, n, Hq, d), const(sign * 6144.0, 1, Hkv, n, d), w)
+    want = np.array([sum(2.0 / (i + 1) for i in range(j, n)) for j in range(n)])
+    _within(_np(w)[0], np.broadcast_to(want, (Hkv, n)), (n + 2 * n + 64) * ref.U32 * want, "weights")
+    c = raas.WeightCache(1, 1, Hq, Hkv, d, n, 8, dtype)
+    c.prefill(0, const(sign * 6144.0, 1, Hkv, n - 1, d), v[None, :, 1:].contiguous())
+    out, w = const(9.0, 1, Hq, d), torch.zeros(1, Hkv, n, device="cuda")
+    c.decode_step(0, const(8192.0, 1, Hq, d), const(sign * 6144.0, 1, Hkv, d), v[None, :, 0].contiguous(), out, weights=w)
+    for h in range(Hkv):
+        mean(_np(out)[0, 2 * h:2 * h + 2], V[h], ("step", h))
+    _within(_np(w)[0], np.full((Hkv, n), 2.0 / n), np.full((Hkv, n), (n + 64) * ref.U32 * 2.0 / n), "step weights")
