@@ -178,8 +178,15 @@ raas_status check_layer(const raas_prefix* p, int32_t layer) {
 // leave the memory-side cache (256 MB) alone: where too little of the layer is
 // still there (us per step, ordinary / non-temporal: 268 MB alone 47.1 / 48.7,
 // in turn with two more caches of that size 58.3 / 52.9; 134 MB 38.0 / 41.8 and
-// 45.8 / 43.4; 67 MB 21.7 / 22.9 and 21.8 / 23.8; 403 MB alone 84.4 / 70.5).
+// 45.8 / 43.4; 67 MB 21.7 / 22.9 and 21.8 / 23.8; 403 MB alone 84.4 / 70.5; with a
+// prefix in front, its attention included: 268 MB and a prefix of 134 MB 100.0 /
+// 90.5, 67 MB and 268 MB 85.0 / 79.6).
 bool non_temporal(double own, double others) { return others + own * 2.0 / 3.0 > 256e6; }
+
+// Bytes of keys and values that attention over a layer of the prefix reads.
+double prefix_bytes(const raas_prefix* p, int32_t layer) {
+    return 2.0 * p->cfg.n_kv_heads * pad_tokens(p->stored[layer], p->bf16) * p->cfg.head_dim * (p->bf16 ? 2 : 4);
+}
 
 // The prefix's attention of `rows` sequences' queries into its parts.
 raas_status prefix_parts(raas_prefix* p, int32_t layer, const void* q, int rows, PrefixView& P, hipStream_t s) {
@@ -199,6 +206,7 @@ raas_status prefix_parts(raas_prefix* p, int32_t layer, const void* q, int rows,
     P.scale_log2 = scale_log2(P.D);
     const hipError_t e = launch_prefix_attention(P, p->bf16, q, s);
     if (e != hipSuccess) return hip_fail(e, "prefix attention launch");
+    if (!capturing(s)) count_streamed(p->device, (unsigned long long)prefix_bytes(p, layer));
     p->last_stream = s;
     return RAAS_OK;
 }
@@ -376,10 +384,11 @@ raas_status raas_weight_step(raas_weight_cache* c, int32_t layer, const void* q,
     }
     // What other layers, caches and pools have read since the layer's last step
     // decides whether it is still in the memory-side cache; a captured step, whose
-    // replays are not seen here, counts the cache's other layers.
+    // replays are not seen here, counts the cache's other layers, and the prefix
+    // as if each of them had one of this length.
     const double own = 2.0 * c->U * c->cpad * c->cfg.head_dim * (c->bf16 ? 2 : 4);
     const bool captured = capturing(s);
-    double others = (c->cfg.n_layers - 1.0) * own;
+    double others = (c->cfg.n_layers - 1.0) * own + (prefix ? c->cfg.n_layers * prefix_bytes(prefix, layer) : 0.0);
     if (!captured) {
         const unsigned long long before = count_streamed(c->device, (unsigned long long)own);
         if (c->streamed_at[layer] != 0) others = (double)(before - c->streamed_at[layer]);

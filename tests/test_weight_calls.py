@@ -1,7 +1,8 @@
 """Calls around the weight cache that other tests leave out: sizes that a query
-must refuse, workspaces of any float alignment."""
+must refuse, workspaces of any float alignment, the count of what is read."""
 from __future__ import annotations
 
+import ctypes
 import os
 
 import pytest
@@ -66,3 +67,50 @@ def test_workspace_of_any_float_alignment(dtype, shift):
                                  torch.cuda.current_stream().cuda_stream)
     torch.cuda.synchronize()
     assert rc == 0 and torch.equal(want, got) and abs(float(got.sum()) - 7.0) < 1e-3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,tokens", [("bf16", 1000), ("f32", 70)])
+def test_reads_of_a_prefix_are_counted(dtype, tokens):
+    """What attention over a prefix reads is counted beside the steps' reads, by
+    which a step tells whether its layer is still in the memory-side cache; a
+    captured call is not."""
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2502_11147_amd as raas
+
+    count = raas.load_library()._ZN4raas14count_streamedEiy
+    count.restype, count.argtypes = ctypes.c_ulonglong, [ctypes.c_int, ctypes.c_ulonglong]
+    B, Hq, Hkv, d, C = 3, 4, 2, 64, 40
+    dt, block = (torch.bfloat16, 32) if dtype == "bf16" else (torch.float32, 16)
+    size = 2 if dtype == "bf16" else 4
+    p = raas.SharedPrefix(2, Hq, Hkv, d, tokens, B, dtype)
+    c = raas.WeightCache(B, 2, Hq, Hkv, d, C, 4, dtype)
+    kv = torch.randn(Hkv, tokens, d, device="cuda").to(dt)
+    q, k = torch.randn(B, Hq, d, device="cuda").to(dt), torch.randn(B, Hkv, d, device="cuda").to(dt)
+    out = torch.empty_like(q)
+    p.store(1, kv, kv)
+    c.prefill(1, None, None)
+    reads = 2 * Hkv * -(-tokens // block) * block * d * size
+    own = 2 * B * Hkv * -(-C // block) * block * d * size
+
+    def counted(call):
+        before = count(0, 0)
+        call()
+        return count(0, 0) - before
+
+    assert counted(lambda: p.attend(1, q, out)) == reads
+    assert counted(lambda: c.decode_step(1, q, k, k, out)) == own
+    assert counted(lambda: c.decode_step(1, q, k, k, out, prefix=p)) == own + reads
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+
+    def capture():
+        with torch.cuda.graph(graph):
+            p.attend(1, q, out)
+            c.decode_step(1, q, k, k, out, prefix=p)
+
+    assert counted(capture) == 0
+    graph.replay()
+    torch.cuda.synchronize()
