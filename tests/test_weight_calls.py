@@ -114,3 +114,38 @@ def test_reads_of_a_prefix_are_counted(dtype, tokens):
     assert counted(capture) == 0
     graph.replay()
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_readme_example():
+    """The README's run of the three together, as it stands there: a private
+    prompt's weights count the shared prompt in front of it, as the steps do."""
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import numpy as np
+
+    import paper_2502_11147_amd as raas
+    import weight_reference as ref
+
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        blocks = f.read().split("```python\n")[1:]
+    (code,) = [b.split("```")[0] for b in blocks if "SharedPrefix" in b]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    mk = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()  # noqa: E731
+    P, S, lens = 90, 200, [90 - i % 20 for i in range(64)]
+    x = dict(raas=raas, k_shared=mk(8, S, 128), v_shared=mk(8, S, 128), q_prompt=mk(64, 64, 32, 128), k_prompt=mk(64, 8, P, 128),
+             v_prompt=mk(64, 8, P, 128), o_prompt=mk(64 * 64, 32, 128), lse=torch.zeros(64 * 64, 32, device="cuda"),
+             w=torch.zeros(64, 8, P, device="cuda"), lens=lens, q=mk(64, 32, 128), k_new=mk(64, 8, 128),
+             v_new=mk(64, 8, 128), out=torch.full((64, 32, 128), float("nan"), device="cuda").bfloat16())
+    exec(code, x)
+    torch.cuda.synchronize()
+    assert torch.isfinite(x["out"].float()).all()
+    f64 = lambda t: t.double().cpu().numpy()  # noqa: E731
+    for b, h in ((0, 0), (63, 7), (19, 3)):
+        n, heads = lens[b], slice(4 * h, 4 * h + 4)
+        Q = f64(x["q_prompt"][b, :, heads])
+        lse = ref.prefix_attention(Q.reshape(-1, 128), f64(x["k_shared"][h]), f64(x["v_shared"][h]), True)
+        want, bound = ref.prompt_weights(Q, f64(x["k_prompt"][b, h, :n]), lse[2].reshape(64, 4))
+        # (the log-sum-exp that the call was given is off by its own bound, and a probability by as much)
+        assert (np.abs(f64(x["w"][b, h, :n]) - want) <= bound + 2 * lse[3].max() * want).all()
