@@ -613,12 +613,16 @@ int share_floats(int G, int parts) { return (G * parts + 3) / 4 * 4; }
 // 22.2).
 constexpr double kFinishBytes = 220e3;
 
-// The fixed part of a step's workgroup in the time of a block, and of a split
-// unit's (us with kSplitBlocks 10 / 20, 8 KV heads: 20 sequences of 2048 tokens
-// 50.8 / 37.3, 24 of 4096 100.5 / 73.5; the one-unit fp32 cache of 256 tokens 9.9
-// / 8.7; with 512 workgroups wanted whatever the rounds, 8 of 2048 28.2 against
-// 21.7 and 16 of 4096 74.9 against 62.2).
-constexpr int kFusedBlocks = 8, kSplitBlocks = 20;
+// What the splits of a unit are chosen by, in us: a workgroup takes a fixed time
+// and its blocks one after the other, each as long as its latency where few
+// workgroups run and as long as its bytes where all do; the end of a unit that is
+// not covered by one workgroup takes more, and more with every head (C 1024 in 4
+// splits against none, 8 units: G 1 11.6 / 11.7, 4 12.3 / 12.0, 7 14.2 / 12.4; in 3,
+// C 900, G 16 17.8 / 13.6).
+constexpr double kFixed = 5.0, kSplitEnd = 2.3, kSplitEndHead = 0.4;
+// a block alone, and its bytes' time with 256 workgroups (16 KB at head_dim 128)
+double block_alone(int D, bool bf16) { return bf16 ? (D == 128 ? 0.12 : 0.08) : (D == 128 ? 0.32 : 0.15); }
+double block_full(int D) { return D == 128 ? 0.62 : 0.31; }
 
 size_t step_lds(int G, int D, int cpad, int nw, bool fused, int parts) {
     return sizeof(float) * ((size_t)nw * 32 + share_floats(G, parts) + (size_t)nw * G * (D + 4) +
@@ -682,14 +686,23 @@ WeightPlan plan_weight_step(int U, int G, int D, int C, bool bf16) {
     // 64.8 / 52.0, 128 of 2048 199.5 / 197.5)
     if (U > 256 && fits(4, 2)) p.waves = 4;
     // Splits: the number that ends soonest when `per` workgroups run at a time
-    // and each takes a fixed part (more of it when the unit is split) besides its
-    // blocks, in units of one block at full load.
+    // (us, one workgroup a unit / split, 8 KV heads of G = 4: 1 sequence of 1024
+    // tokens 12.0 / 12.3, of 2048 16.0 / 12.7, 4 of 2048 18.9 / 15.6, 16 of 1024 17.3 /
+    // 21.0, 16 of 2048 26.8 / 32.6, 19 of 4963 72.1 / 92.5, 82 of 2760 174 / 210; 4 KV
+    // heads of G = 7, 32 of 3201 39.0 / 55.0).
     const int per = p.waves == 8 ? 256 : 512;
     int want = 1;
     double best = 0.0;
+    // (a layer beyond the memory-side cache: its blocks take longer to come)
+    const double alone = block_alone(D, bf16) + (2.0 * U * cpad * D * (bf16 ? 2 : 4) > 256e6 ? 0.08 : 0.0);
     for (int ns = 1; ns <= kMaxStepSplits && (ns == 1 || nb >= ns * p.waves); ++ns) {
-        const double rounds = ((long long)U * ns + per - 1) / per;
-        const double cost = rounds * ((nb + ns - 1) / ns + (ns > 1 ? kSplitBlocks : kFusedBlocks));
+        const double end = ns == 1 && fits(p.waves, 1) ? 0.0 : kSplitEnd + kSplitEndHead * G;
+        auto round = [&](long long workgroups) {
+            const double full = block_full(D) * workgroups / 256;
+            return (nb + ns - 1) / ns * std::max(alone + 0.58 * full, full) + kFixed + end;
+        };
+        const long long all = (long long)U * ns, rest = all % per;
+        const double cost = all / per * round(per) + (rest > 0 ? round(rest) : 0.0);
         if (ns == 1 || cost < best) {
             best = cost;
             want = ns;
