@@ -60,6 +60,14 @@ raas_status check_heads(int n_q_heads, int n_kv_heads, int head_dim, int dtype) 
     return RAAS_OK;
 }
 
+// Bytes that no device has; sizes below it do not overflow.
+constexpr double kNoDevice = 1e17;
+raas_status check_bytes(double layers, double units, double tokens, int head_dim, bool bf16) {
+    const double bytes = 2.0 * layers * units * tokens * head_dim * (bf16 ? 2 : 4);
+    if (bytes > kNoDevice) return fail(RAAS_E_OOM, "keys and values of %.3g bytes fit no device", bytes);
+    return RAAS_OK;
+}
+
 // A part of a handle's memory; `clear`: it starts at zero.
 struct Req {
     void** ptr;
@@ -258,6 +266,9 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
     if (cfg->recent < 0 || cfg->recent >= cfg->capacity)
         return fail(RAAS_E_INVALID, "recent must lie in [0, capacity) (got %d)", cfg->recent);
     if ((double)cfg->batch * cfg->n_kv_heads > 1e6) return fail(RAAS_E_INVALID, "batch * n_kv_heads too large");
+    const raas_status sb = check_bytes(cfg->n_layers, (double)cfg->batch * cfg->n_kv_heads, cfg->capacity, cfg->head_dim,
+                                       cfg->dtype == RAAS_BF16);
+    if (sb != RAAS_OK) return sb;
     raas_weight_cache* c = nullptr;
     try {
         c = new raas_weight_cache();
@@ -446,6 +457,9 @@ raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas
     if (cfg->max_rows < 1 || (double)cfg->max_rows * cfg->n_q_heads > kMaxQueries)
         return fail(RAAS_E_INVALID, "max_rows must be >= 1, and max_rows * n_q_heads at most %d (got %d rows)", kMaxQueries,
                     cfg->max_rows);
+    const raas_status sb =
+        check_bytes(cfg->n_layers, cfg->n_kv_heads, cfg->max_tokens, cfg->head_dim, cfg->dtype == RAAS_BF16);
+    if (sb != RAAS_OK) return sb;
     raas_prefix* p = nullptr;
     try {
         p = new raas_prefix();

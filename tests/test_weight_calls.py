@@ -1,5 +1,6 @@
 """Calls around the weight cache that other tests leave out: sizes that a query
-must refuse, workspaces of any float alignment, the count of what is read."""
+must refuse, handles past 64 bits, workspaces of any float alignment, the count
+of what is read, the README's example."""
 from __future__ import annotations
 
 import ctypes
@@ -40,6 +41,27 @@ def test_workspace_of_refused_sizes_is_zero(lib, sizes):
 def test_workspace_of_allowed_sizes(lib, sizes):
     assert lib.raas_prompt_weights_workspace(*sizes) > 0
     assert lib.raas_prompt_weights_workspace(*sizes[:3], 0, 1) == 0  # nothing to do
+
+
+# sizes of which the product, or that of the keys alone, is 0 or small modulo 2^64
+@pytest.mark.parametrize("layers,kv_heads", [(1 << 20, 32768), ((1 << 20) + 1, 32768), (1 << 21, 32768), (1 << 19, 65535)])
+def test_prefix_of_more_bytes_than_64_bits_count(lib, layers, kv_heads):
+    import paper_2502_11147_amd as raas
+
+    cfg = raas.PrefixConfig(layers, kv_heads, kv_heads, 128, 1 << 20, 1, raas.F32)
+    h = ctypes.c_void_p()
+    assert lib.raas_create_prefix(ctypes.byref(cfg), None, ctypes.byref(h)) == raas.E_OOM
+    assert not h.value and b"bytes" in lib.raas_last_error()
+
+
+@pytest.mark.parametrize("layers,batch", [(1 << 16, 1 << 19), (1 << 20, 1 << 15)])
+def test_cache_of_more_bytes_than_64_bits_count(lib, layers, batch):
+    import paper_2502_11147_amd as raas
+
+    cfg = raas.WeightConfig(batch, layers, 1, 1, 128, 1 << 20, 0, raas.F32)
+    h = ctypes.c_void_p()
+    assert lib.raas_create_weight_cache(ctypes.byref(cfg), None, ctypes.byref(h)) == raas.E_OOM
+    assert not h.value and b"bytes" in lib.raas_last_error()
 
 
 @pytest.mark.gpu
