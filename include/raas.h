@@ -328,7 +328,8 @@ typedef struct raas_prefix raas_prefix; /* opaque */
 
 /* Validates cfg, allocates the cache in device memory and clears its records on
  * `stream`. The caller releases it with raas_destroy_weight_cache. Errors:
- * RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_HIP. */
+ * RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_STATE (the stream is being captured),
+ * RAAS_E_HIP. */
 raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream, raas_weight_cache** out);
 
 /* Synchronises the cache's last stream and frees it. NULL is ignored. */

@@ -68,6 +68,13 @@ raas_status check_bytes(double layers, double units, double tokens, int head_dim
     return RAAS_OK;
 }
 
+// A captured creation would clear its records only when the graph runs.
+raas_status check_creation(void* stream) {
+    if (capturing((hipStream_t)stream))
+        return fail(RAAS_E_STATE, "a handle cannot be created on a stream that is being captured");
+    return RAAS_OK;
+}
+
 // A part of a handle's memory; `clear`: it starts at zero.
 struct Req {
     void** ptr;
@@ -269,6 +276,8 @@ raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream
     const raas_status sb = check_bytes(cfg->n_layers, (double)cfg->batch * cfg->n_kv_heads, cfg->capacity, cfg->head_dim,
                                        cfg->dtype == RAAS_BF16);
     if (sb != RAAS_OK) return sb;
+    const raas_status sc = check_creation(stream);
+    if (sc != RAAS_OK) return sc;
     raas_weight_cache* c = nullptr;
     try {
         c = new raas_weight_cache();
@@ -460,6 +469,8 @@ raas_status raas_create_prefix(const raas_prefix_config* cfg, void* stream, raas
     const raas_status sb =
         check_bytes(cfg->n_layers, cfg->n_kv_heads, cfg->max_tokens, cfg->head_dim, cfg->dtype == RAAS_BF16);
     if (sb != RAAS_OK) return sb;
+    const raas_status sc = check_creation(stream);
+    if (sc != RAAS_OK) return sc;
     raas_prefix* p = nullptr;
     try {
         p = new raas_prefix();

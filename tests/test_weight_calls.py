@@ -171,3 +171,62 @@ def test_readme_example():
         want, bound = ref.prompt_weights(Q, f64(x["k_prompt"][b, h, :n]), lse[2].reshape(64, 4))
         # (the log-sum-exp that the call was given is off by its own bound, and a probability by as much)
         assert (np.abs(f64(x["w"][b, h, :n]) - want) <= bound + 2 * lse[3].max() * want).all()
+
+
+def _gpu():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2502_11147_amd as raas
+
+    return torch, raas
+
+
+@pytest.mark.gpu
+def test_no_handle_is_created_during_capture():
+    torch, raas = _gpu()
+    x = torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, capture_error_mode="relaxed"):
+        x += 1.0
+        for make in (lambda: raas.WeightCache(1, 1, 4, 1, 64, 40, 4), lambda: raas.SharedPrefix(1, 4, 1, 64, 40, 4)):
+            with pytest.raises(raas.RaasError) as e:
+                make()
+            assert e.value.code == raas.E_STATE
+    graph.replay()  # the capture went on
+    torch.cuda.synchronize()
+    assert (x == 1.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [2, 20, 70])
+def test_prefix_replays_over_other_lengths(rows):
+    """A captured call keeps the number of parts of its capture, whatever is
+    stored when it is replayed: longer, shorter, nothing, with and between eager
+    calls."""
+    torch, raas = _gpu()
+    Hq, Hkv, d = 4, 2, 128
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    mk = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()  # noqa: E731
+    p = raas.SharedPrefix(1, Hq, Hkv, d, 3000, rows)
+    q, out, want = mk(rows, Hq, d), mk(rows, Hq, d), mk(rows, Hq, d)
+    lse, lse_want = torch.zeros(rows, Hq, device="cuda"), torch.zeros(rows, Hq, device="cuda")
+    p.store(0, mk(Hkv, 1500, d), mk(Hkv, 1500, d))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        p.attend(0, q, out, lse)
+    for n in (1500, 3000, 17, 0, 1, 33, 0, 2999):
+        k, v = (mk(Hkv, n, d), mk(Hkv, n, d)) if n else (None, None)
+        p.store(0, k, v)
+        out.fill_(5.0)
+        for _ in range(2):
+            graph.replay()
+        p.attend(0, q, want, lse_want)
+        torch.cuda.synchronize()
+        if n == 0:
+            assert (out == 0).all() and (lse == -float("inf")).all()
+        # (one bf16 rounding of either; the parts are added in another order)
+        assert ((out.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-5).all(), n
+        assert n == 0 or ((lse - lse_want).abs() <= 1e-5 * (1.0 + lse_want.abs())).all(), n
