@@ -360,7 +360,8 @@ raas_status raas_weight_prefill(raas_weight_cache* cache, int32_t layer, const v
  *   weights_out   [u][capacity]: its weight (fp32), 0 if free;
  *   evicted_out   [u]          : position of the token that this step evicted, or -1.
  * active: optional DEVICE int32 [batch]; sequences with a zero entry take no
- * step: their state and rows of the outputs stay as they are. prefix: NULL, or
+ * step: their state and rows of the outputs stay as they are (attention over a
+ * prefix is computed for the whole batch all the same). prefix: NULL, or
  * a shared prefix of the same heads, head_dim, dtype and device, whose layer of
  * the same index has been stored and whose max_rows covers the batch (its
  * scratch is used: the call counts as one of the prefix's too). Errors:

@@ -324,11 +324,12 @@ __global__ __launch_bounds__(256) void k_prefix_join(PrefixView P, T* __restrict
 
 // Wavefronts of the kernel for many rows; 0: the one for few, which reads the
 // prefix once per 32 rows but needs no step of all wavefronts per block (us, few
-// / many: 48 rows of 8 KV heads, 32768 tokens 34.2 / 43.1, 64 rows, 4096 tokens
-// 15.4 / 14.1, 128 rows 24.9 / 22.7, 128 rows and 32768 tokens 92.5 / 48.8).
+// / many, 8 KV heads: 48 rows, 32768 tokens 32.4 / 35.6, 64 rows 32.6 / 35.2 and
+// with 4096 tokens 14.9 / 12.2, 128 rows, 4096 tokens 15.4 / 15.6).
 // Four where eight would leave half a tile empty (us, 8 / 4 wavefronts: 368 rows
-// of 4 KV heads, 8520 tokens, fp32 87.0 / 72.7, bf16 25.5 / 26.1, 896 rows of 2
-// with a step 61.0 / 56.9).
+// of 4 KV heads, 8520 tokens, fp32 87.6 / 73.9, bf16 28.0 / 28.0; 8 KV heads, bf16,
+// 128 rows, 4096 tokens 17.3 / 15.5, 124 rows, 8520 tokens 23.0 / 21.7, 384 rows,
+// 20000 tokens 63.5 / 58.4).
 int wide(int rows) { return rows <= 64 ? 0 : (rows + 127) / 128 % 2 == 1 ? 4 : 8; }
 // rows of a workgroup's tile, and the tiles
 int row_tile(int rows) { return wide(rows) ? wide(rows) * 16 * kWideTiles : rows <= 16 ? 16 : 32; }
@@ -370,15 +371,15 @@ int plan_prefix(int nkv, int rows, int tokens, bool bf16) {
         // A part takes the time of its blocks, one after the other, and writing and
         // joining its rows takes that of a bf16 block per 4096 rows of all heads:
         // the least of nb / parts + parts * rows / 4096 (us with parts of 8 / 4 blocks
-        // / by this rule, 8 KV heads of G = 4: 40 sequences over 700 tokens 15.8 / 13.1
-        // / 12.6, 64 over 1024 18.2 / 16.1 / 16.2, 32 over 8192 18.4 / 24.0 / 18.6; an
+        // / by this rule, 8 KV heads of G = 4: 40 sequences over 700 tokens 18.1 / 14.2
+        // / 13.4, 64 over 1024 20.3 / 16.7 / 16.7, 32 over 8192 19.5 / 25.0 / 19.6; an
         // fp32 block is half the tokens at eight times the work: 124 rows, 270 tokens
-        // 14.4, with parts of 8 blocks 22.6).
+        // 13.8, with parts of 8 / 4 blocks 22.5 / 18.5).
         parts = (int)lround(sqrt((double)nb * (bf16 ? 4096 : 16384) / ((double)nkv * rows)));
     } else {
-        // two blocks per wavefront (us with 1 / 2 / 4: 32 rows, 8192 tokens 23.1 / 19.9
-        // / 20.3, 16 rows, 4096 tokens 11.8 / 11.6 / 12.9); of fp32, half the tokens at
-        // eight times the work, one (40 rows, 2000 tokens: 23.4, with two 25.9)
+        // two blocks per wavefront (us with 1 / 2 / 4: 32 rows, 8192 tokens 16.6 / 16.0
+        // / 18.4, 16 rows, 4096 tokens 11.8 / 11.2 / 12.1); of fp32, half the tokens at
+        // eight times the work, one (40 rows, 2000 tokens: 22.6, with two 25.6)
         const int least = bf16 ? 2 * kWaves : kWaves;
         parts = (nb + least - 1) / least;
     }
