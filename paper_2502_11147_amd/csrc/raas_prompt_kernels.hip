@@ -132,9 +132,10 @@ __global__ __launch_bounds__(kThreads) void k_prompt_join(PromptView v, SeqLens 
 // workgroups that follow each other have equal work, and with eight units each
 // XCD's L2 serves one (row tiles first, some shader engines always got the long
 // ones: 125 us for 100). KW wavefronts share RT tiles of 16 rows and take a part
-// of the staged keys each. LDS bounds it besides the exponentials (it gives a CU
-// some 60 bytes a cycle): the more rows a wavefront holds, the fewer of its
-// reads a product takes.
+// of the staged keys each. Bound by the vector instructions (62 % of the cycles,
+// a prompt of 4096 tokens, every query) and the products (35 %), which follow each
+// other; LDS moves 28 bytes a cycle. The more rows a wavefront holds, the fewer
+// of its reads a product takes.
 template <typename T, int D, int RT, int KW>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void k_prompt_rows(PromptView v,
                                                                                                    SeqLens lens) {
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
 // tiles (the ones that most rows see first), row chunks. A wavefront holds kHeld
 // tiles of 16 keys; the rows pass through LDS with their maximum (base 2) and the
 // inverse of their sum.
-// Bound as the kernel above. Three wavefronts per SIMD at head_dim 64, where two
+// Bound as the kernel above (52 and 29 %). Three wavefronts per SIMD at head_dim 64, where two
 // registers too many would leave two (a whole prompt of 3000 tokens 94.6 us, 97).
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void k_prompt_keys(
