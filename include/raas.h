@@ -425,6 +425,107 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
                                 int32_t max_len, int32_t window, float* weights, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * A cache of every token in 4 or 8 bits a value, in pages that the caller hands
+ * out: what RaaS saves by holding fewer tokens it saves by holding fewer bits.
+ * A group of 32 consecutive channels of a token's key or value shares a power of
+ * two X, the least with max |x| < 7 X in 4 bits (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives) and < 464 X in 8 (e4m3, up to 448); each value becomes the
+ * nearest such number times X, of two equally near the one with the even code.
+ * (X lies within 2^-111 .. 2^125 and 2^119: groups below 2^-109 lose digits, the
+ * largest numbers saturate. A group that holds an infinity or NaN reads as NaN.)
+ * A token takes head_dim * (key_bits + value_bits) / 8 + head_dim / 16 bytes per
+ * KV head.
+ *
+ * A page holds page_size tokens of every KV head of a layer. Calls name the pages
+ * of their sequences in `table`, DEVICE int32 [batch][table_width]: token t of
+ * sequence b lies in page table[b][t / page_size], one of 0 .. n_pages - 1; every
+ * layer has pages of its own under the same numbers. Sequences may share pages that
+ * none of them writes. Tokens whose entry is no page, or that lie past the table's
+ * row, are neither written, read nor attended to. Tokens that were never written
+ * hold anything. Table, lengths and counts are read when the call runs, so that
+ * calls may be captured into a HIP graph: a replay works on what they hold then.
+ *
+ * The conventions at the top hold: device tensors (aligned to their element type),
+ * nothing awaited (but by the destroy), finite inputs (scaled logits within 5e8 of
+ * 0, as above), calls on one handle, and graphs of them, ordered (attention and
+ * steps share its scratch). Nothing is allocated after the creation. The same calls
+ * on the same contents give the same bits. A handle's calls run on the device that
+ * was current at its creation. */
+typedef struct {
+    int32_t n_layers;    /* >= 1 */
+    int32_t n_q_heads;   /* multiple of n_kv_heads, group G = n_q_heads/n_kv_heads <= 16 */
+    int32_t n_kv_heads;  /* 1 .. 65535 */
+    int32_t head_dim;    /* 64 or 128 */
+    int32_t page_size;   /* tokens per page: 32, 64, 128 or 256 */
+    int32_t n_pages;     /* pages of a layer, >= 1 */
+    int32_t max_batch;   /* sequences per call, 1 .. 4096 */
+    int32_t max_queries; /* queries per sequence of raas_quant_attention, >= 1;
+                            max_batch * max_queries * n_q_heads <= 16777216 */
+    int32_t key_bits;    /* 4 or 8 */
+    int32_t value_bits;  /* 4 or 8 */
+    int32_t dtype;       /* raas_dtype of q, k, v and out */
+} raas_quant_config;
+
+typedef struct raas_quant_cache raas_quant_cache; /* opaque */
+
+/* Validates cfg and allocates the cache in device memory. The caller releases it
+ * with raas_destroy_quant_cache. Errors: RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_STATE
+ * (the stream is being captured), RAAS_E_HIP. */
+raas_status raas_create_quant_cache(const raas_quant_config* cfg, void* stream, raas_quant_cache** out);
+
+/* Synchronises the cache's last stream and frees it. NULL is ignored. */
+void raas_destroy_quant_cache(raas_quant_cache* cache);
+
+/* Device bytes the cache holds; fixed from creation on. */
+size_t raas_quant_cache_bytes(const raas_quant_cache* cache);
+
+/* Quantises and stores tokens: rows 0 .. counts[b] - 1 of k, v
+ * [batch][n_kv_heads][max_tokens][head_dim] become tokens start[b] .. of sequence
+ * b. start, counts: DEVICE int32 [batch]; counts NULL, or an entry above
+ * max_tokens: max_tokens; a sequence whose count is not positive or whose start is
+ * negative stores nothing. table_width: 1 .. 1048576 / page_size. Errors:
+ * RAAS_E_INVALID, RAAS_E_HIP. */
+raas_status raas_quant_write(raas_quant_cache* cache, int32_t layer, const void* k, const void* v, const int32_t* table,
+                             int32_t table_width, const int32_t* start, const int32_t* counts, int32_t batch,
+                             int32_t max_tokens, void* stream);
+
+/* The inverse: the same rows of k, v receive the values that tokens start[b] ..
+ * are held as (exact in either dtype); other rows stay as they are. Errors as
+ * raas_quant_write. */
+raas_status raas_quant_read(raas_quant_cache* cache, int32_t layer, void* k, void* v, const int32_t* table,
+                            int32_t table_width, const int32_t* start, const int32_t* counts, int32_t batch,
+                            int32_t max_tokens, void* stream);
+
+/* Causal softmax attention (scale 1/sqrt(head_dim)) of the last counts[b] of the
+ * lens[b] tokens that sequence b holds, their own among them: query i of q
+ * [batch][queries][n_q_heads][head_dim] is that of token lens[b] - counts[b] + i and
+ * sees the tokens up to it. lens, counts: DEVICE int32 [batch]; counts NULL, or an
+ * entry above `queries`: queries; lens past the table's row count as its end. out
+ * like q, and, unless NULL, lse [batch][queries][n_q_heads] (fp32): the natural
+ * logarithm of the sum of the exponentials of the scaled logits. A query that sees
+ * no token has out 0 and lse -inf. Rows from counts[b] on, and those of sequences
+ * of negative length, stay as they are. Errors: RAAS_E_INVALID, RAAS_E_HIP. */
+raas_status raas_quant_attention(raas_quant_cache* cache, int32_t layer, const void* q, const int32_t* table,
+                                 int32_t table_width, const int32_t* lens, const int32_t* counts, int32_t batch,
+                                 int32_t queries, void* out, float* lse, void* stream);
+
+/* One decode step: stores the new token of each sequence as raas_quant_write
+ * would, at position lens[b] (DEVICE int32 [batch]: the tokens held so far;
+ * negative: the sequence takes no step, its rows of the outputs stay as they are),
+ * and attends from q [batch][n_q_heads][head_dim] to all lens[b] + 1 tokens. k_new,
+ * v_new [batch][n_kv_heads][head_dim]; out like q. Optional outputs (NULL = not
+ * written): lse [batch][n_q_heads] as above; k_held, v_held like k_new, the new
+ * token as it is now held (left as they are for a token that finds no page, which
+ * is not attended to either). prefix: NULL, or a shared prefix of the same heads,
+ * head_dim, dtype and device, whose layer of the same index has been stored and
+ * whose max_rows covers the batch, to which every query attends besides (its
+ * scratch is used: the call counts as one of the prefix's too). The caller counts
+ * lens up. Errors: RAAS_E_INVALID, RAAS_E_STATE (prefix not stored), RAAS_E_HIP. */
+raas_status raas_quant_step(raas_quant_cache* cache, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                            const int32_t* table, int32_t table_width, const int32_t* lens, int32_t batch, void* out,
+                            float* lse, void* k_held, void* v_held, raas_prefix* prefix, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,7 +30,8 @@ EXPORTS = (
     "raas_create_weight_cache", "raas_destroy_weight_cache", "raas_weight_cache_bytes", "raas_weight_prefill",
     "raas_weight_step", "raas_weight_export_state", "raas_create_prefix", "raas_destroy_prefix",
     "raas_prefix_bytes", "raas_prefix_store", "raas_prefix_attention", "raas_prompt_weights_workspace",
-    "raas_prompt_weights",
+    "raas_prompt_weights", "raas_create_quant_cache", "raas_destroy_quant_cache", "raas_quant_cache_bytes",
+    "raas_quant_write", "raas_quant_read", "raas_quant_attention", "raas_quant_step",
 )
 
 
@@ -121,7 +122,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             ("raas_prefix_store", i32, vp, i32, vp, vp, i32, vp),
             ("raas_prefix_attention", i32, vp, i32, vp, i32, vp, vp, vp),
             ("raas_prompt_weights_workspace", size, i32, i32, i32, i32, i32),
-            ("raas_prompt_weights", i32, i32, i32, i32, i32, i32, vp, vp, vp, ip, i32, i32, vp, vp, size, vp)):
+            ("raas_prompt_weights", i32, i32, i32, i32, i32, i32, vp, vp, vp, ip, i32, i32, vp, vp, size, vp),
+            ("raas_create_quant_cache", i32, vp, vp, ctypes.POINTER(vp)),
+            ("raas_destroy_quant_cache", None, vp),
+            ("raas_quant_cache_bytes", size, vp),
+            ("raas_quant_write", i32, vp, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp),
+            ("raas_quant_read", i32, vp, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp),
+            ("raas_quant_attention", i32, vp, i32, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp),
+            ("raas_quant_step", i32, vp, i32, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp)):
         function = getattr(lib, name)
         function.restype, function.argtypes = restype, argtypes
     _lib = lib
@@ -327,3 +335,4 @@ class Pool:
 
 
 from .weight_cache import PrefixConfig, SharedPrefix, WeightCache, WeightConfig, prompt_weights  # noqa: E402,F401
+from .quant_cache import QuantCache, QuantConfig  # noqa: E402,F401

@@ -1,6 +1,6 @@
-// What the kernels of the weight cache, the shared prefix and the prompt
-// weights have in common: the layout of a block of tokens in memory, and the
-// products on the matrix cores.
+// What the kernels of the weight cache, the shared prefix, the prompt weights and
+// the quantised cache have in common: the layout of a block of tokens in memory,
+// the products on the matrix cores, the hand-over between workgroups.
 //
 // A block is the tokens of 64 16-byte reads per 16 channels of values: 32
 // tokens in bf16, 16 in fp32. Keys and values are stored in the order in which
@@ -271,6 +271,45 @@ __device__ __forceinline__ void attend(const u32x4 (&kr)[D / 16], const u32x4 (&
 __device__ __forceinline__ uint32_t float_key(float x) {
     const uint32_t b = __float_as_uint(x);
     return (b >> 31) ? ~b : b | 0x80000000u;
+}
+
+// Hand-over between workgroups of one launch. The XCDs' L2s are not coherent
+// with each other, so what crosses is written through and read past them (agent
+// scope); once a wavefront's stores are acknowledged every XCD reads them.
+template <typename T>
+__device__ __forceinline__ void publish(T* p, T v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T published(const T* p) {
+    return __hip_atomic_load(const_cast<T*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void publish4(float* p, f32x4 v) {  // p: 16-byte aligned
+    unsigned long long* q = reinterpret_cast<unsigned long long*>(p);
+    publish(q, (unsigned long long)__float_as_uint(v[1]) << 32 | __float_as_uint(v[0]));
+    publish(q + 1, (unsigned long long)__float_as_uint(v[3]) << 32 | __float_as_uint(v[2]));
+}
+__device__ __forceinline__ f32x4 published4(const float* p) {
+    const unsigned long long* q = reinterpret_cast<const unsigned long long*>(p);
+    const unsigned long long x = published(q), y = published(q + 1);
+    return f32x4{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)), __uint_as_float((uint32_t)y),
+                 __uint_as_float((uint32_t)(y >> 32))};
+}
+// True on the last of `total` workgroups to call it for this counter, once all
+// that they published is readable; the counter is zero again afterwards. No
+// workgroup waits for another.
+__device__ __forceinline__ bool arrive_last(int32_t* counter, int total) {
+    __shared__ int s_last;
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == total - 1) publish(counter, 0);
+        s_last = before == total - 1;
+    }
+    __syncthreads();
+    return s_last != 0;
 }
 
 }  // namespace blk

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "raas.h"
+
 namespace raas {
 
 // Per-unit record of a weight cache:
@@ -99,6 +101,15 @@ hipError_t launch_prefix_store(void* K, void* V, int32_t* len, int nkv, int D, i
                                const void* v, int tokens, hipStream_t s);
 hipError_t launch_prefix_attention(const PrefixView& P, bool bf16, const void* q, hipStream_t s);
 hipError_t launch_prefix_join(const PrefixView& P, bool bf16, void* out, float* lse, hipStream_t s);
+
+// A cache whose step attends to a shared prefix besides, and the refusals that
+// follow; then the prefix's attention of the step's queries into its parts.
+struct PrefixUser {
+    int n_q_heads, n_kv_heads, head_dim, dtype, device, batch;
+};
+raas_status check_step_prefix(const raas_prefix* p, int32_t layer, const PrefixUser& u);
+raas_status step_prefix_parts(raas_prefix* p, int32_t layer, const void* q, int batch, PrefixParts& parts,
+                              hipStream_t s);
 
 // Keys and values of units to blocks: row t of unit u comes from row
 // pos[u * pad + t] of its source (pos NULL: row t), for t < min(len, C).

@@ -226,46 +226,6 @@ __global__ __launch_bounds__(256) void k_store(T* __restrict__ K, T* __restrict_
 __global__ void k_set_int(int32_t* p, int32_t v) { *p = v; }
 
 // ---------------------------------------------------------------------------
-// Hand-over between workgroups of one launch. The XCDs' L2s are not coherent
-// with each other, so what crosses is written through and read past them (agent
-// scope); once a wavefront's stores are acknowledged every XCD reads them.
-template <typename T>
-__device__ __forceinline__ void publish(T* p, T v) {
-    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-template <typename T>
-__device__ __forceinline__ T published(const T* p) {
-    return __hip_atomic_load(const_cast<T*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void publish4(float* p, f32x4 v) {  // p: 16-byte aligned
-    unsigned long long* q = reinterpret_cast<unsigned long long*>(p);
-    publish(q, (unsigned long long)__float_as_uint(v[1]) << 32 | __float_as_uint(v[0]));
-    publish(q + 1, (unsigned long long)__float_as_uint(v[3]) << 32 | __float_as_uint(v[2]));
-}
-__device__ __forceinline__ f32x4 published4(const float* p) {
-    const unsigned long long* q = reinterpret_cast<const unsigned long long*>(p);
-    const unsigned long long x = published(q), y = published(q + 1);
-    return f32x4{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)), __uint_as_float((uint32_t)y),
-                 __uint_as_float((uint32_t)(y >> 32))};
-}
-// True on the last of `total` workgroups to call it for this counter, once all
-// that they published is readable; the counter is zero again afterwards. No
-// workgroup waits for another.
-__device__ __forceinline__ bool arrive_last(int32_t* counter, int total) {
-    __shared__ int s_last;
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (before == total - 1) publish(counter, 0);
-        s_last = before == total - 1;
-    }
-    __syncthreads();
-    return s_last != 0;
-}
-
-// ---------------------------------------------------------------------------
 // The end of a step: from the maxima and sums (ml) and unnormalised outputs (o)
 // of `nsrc` disjoint parts of the held tokens, and those of the prefix, the
 // output (if j_lo is 0); from the logits (x4: those of four tokens) the weights

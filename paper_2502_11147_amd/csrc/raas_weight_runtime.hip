@@ -1,7 +1,6 @@
 // Host runtime of the weight cache, the shared prefix and the prompt weights:
 // argument checks, their memory, and the launches on the caller's stream.
 // Implements the second half of include/raas.h.
-#include <math.h>
 #include <string.h>
 
 #include <algorithm>
@@ -9,104 +8,15 @@
 #include <vector>
 
 #include "raas.h"
-#include "raas_host.h"
+#include "raas_handle.h"
 #include "raas_weight_internal.h"
 
 using namespace raas;
 
 namespace {
 
-// Tokens that a unit of a cache, a prefix or a prompt may have.
-constexpr int kMaxTokens = 1 << 20;
 // Query rows of one call over a prefix, and of one KV head's window (the grids' limits).
 constexpr int kMaxQueries = 1 << 17, kMaxWindowRows = 1 << 23;
-
-// The handle's device for the length of a call.
-class DeviceScope {
-  public:
-    explicit DeviceScope(int device) {
-        if (hipGetDevice(&before_) != hipSuccess) before_ = -1;
-        if (before_ != device) error_ = hipSetDevice(device);
-        else before_ = -1;
-    }
-    ~DeviceScope() {
-        if (before_ >= 0) (void)hipSetDevice(before_);
-    }
-    DeviceScope(const DeviceScope&) = delete;
-    DeviceScope& operator=(const DeviceScope&) = delete;
-    hipError_t error() const { return error_; }
-
-  private:
-    int before_ = -1;
-    hipError_t error_ = hipSuccess;
-};
-
-float scale_log2(int d) { return (float)(1.4426950408889634 / sqrt((double)d)); }
-int block_tokens(bool bf16) { return bf16 ? 32 : 16; }
-int pad_tokens(int n, bool bf16) { return (n + block_tokens(bf16) - 1) / block_tokens(bf16) * block_tokens(bf16); }
-
-// The layer's shape, as every one of these calls takes it.
-raas_status check_heads(int n_q_heads, int n_kv_heads, int head_dim, int dtype) {
-    if (n_kv_heads < 1 || n_kv_heads > 65535)
-        return fail(RAAS_E_INVALID, "n_kv_heads must lie in [1, 65535] (got %d)", n_kv_heads);
-    if (n_q_heads < 1 || n_q_heads % n_kv_heads != 0)
-        return fail(RAAS_E_INVALID, "n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)", n_q_heads,
-                    n_kv_heads);
-    if (n_q_heads / n_kv_heads > 16)
-        return fail(RAAS_E_INVALID, "query group n_q_heads/n_kv_heads = %d exceeds 16", n_q_heads / n_kv_heads);
-    if (head_dim != 64 && head_dim != 128) return fail(RAAS_E_INVALID, "head_dim must be 64 or 128 (got %d)", head_dim);
-    if (dtype != RAAS_F32 && dtype != RAAS_BF16)
-        return fail(RAAS_E_INVALID, "dtype must be RAAS_F32 or RAAS_BF16 (got %d)", dtype);
-    return RAAS_OK;
-}
-
-// Bytes that no device has; sizes below it do not overflow.
-constexpr double kNoDevice = 1e17;
-raas_status check_bytes(double layers, double units, double tokens, int head_dim, bool bf16) {
-    const double bytes = 2.0 * layers * units * tokens * head_dim * (bf16 ? 2 : 4);
-    if (bytes > kNoDevice) return fail(RAAS_E_OOM, "keys and values of %.3g bytes fit no device", bytes);
-    return RAAS_OK;
-}
-
-// A captured creation would clear its records only when the graph runs.
-raas_status check_creation(void* stream) {
-    if (capturing((hipStream_t)stream))
-        return fail(RAAS_E_STATE, "a handle cannot be created on a stream that is being captured");
-    return RAAS_OK;
-}
-
-// A part of a handle's memory; `clear`: it starts at zero.
-struct Req {
-    void** ptr;
-    size_t bytes;
-    bool clear;
-};
-
-// One allocation, cut into parts of 256 bytes and up (an allocation takes some
-// 30 us); what must start at zero is cleared on the stream. Keys, values and
-// scratch need not: no place is looked at before it is written, but for the rest
-// of a block, whose logits and values are masked.
-raas_status allocate(const std::vector<Req>& reqs, void** base, size_t& total, hipStream_t s) {
-    auto padded = [](size_t n) { return (n + 255) & ~(size_t)255; };
-    total = 0;
-    for (const Req& r : reqs) total += padded(r.bytes);
-    hipError_t e = hipMalloc(base, total);
-    if (e != hipSuccess) {
-        *base = nullptr;
-        (void)hipGetLastError();
-        return fail(e == hipErrorOutOfMemory ? RAAS_E_OOM : RAAS_E_HIP, "hipMalloc(%zu bytes): %s", total,
-                    hipGetErrorString(e));
-    }
-    char* at = (char*)*base;
-    for (const Req& r : reqs) {
-        *r.ptr = at;
-        at += padded(r.bytes);
-        if (!r.clear) continue;
-        e = hipMemsetAsync(*r.ptr, 0, r.bytes, s);
-        if (e != hipSuccess) return hip_fail(e, "hipMemsetAsync");
-    }
-    return RAAS_OK;
-}
 
 // Lengths of sequences seq0 .. of a launch: lens (NULL: max_len), -1 where the mask leaves one out.
 int fill_lens(SeqLens& out, const int32_t* lens, const int32_t* mask, int max_len, int seq0, int nseq) {
@@ -259,6 +169,30 @@ raas_status check_prompt(int batch, int n_q_heads, int n_kv_heads, int head_dim,
 
 }  // namespace
 
+namespace raas {
+
+raas_status check_step_prefix(const raas_prefix* p, int32_t layer, const PrefixUser& u) {
+    const raas_prefix_config& f = p->cfg;
+    if (f.n_q_heads != u.n_q_heads || f.n_kv_heads != u.n_kv_heads || f.head_dim != u.head_dim || f.dtype != u.dtype)
+        return fail(RAAS_E_INVALID, "the prefix has other heads or another type than the cache");
+    if (p->device != u.device) return fail(RAAS_E_INVALID, "the prefix lies on another device");
+    if (layer >= f.n_layers) return fail(RAAS_E_INVALID, "the prefix has no layer %d", layer);
+    if (p->stored[layer] < 0) return fail(RAAS_E_STATE, "layer %d of the prefix has not been stored", layer);
+    if (u.batch > f.max_rows)
+        return fail(RAAS_E_INVALID, "batch %d exceeds the prefix's max_rows %d", u.batch, f.max_rows);
+    return RAAS_OK;
+}
+
+raas_status step_prefix_parts(raas_prefix* p, int32_t layer, const void* q, int batch, PrefixParts& parts,
+                              hipStream_t s) {
+    PrefixView P;
+    const raas_status st = prefix_parts(p, layer, q, batch, P, s);
+    if (st == RAAS_OK) parts = PrefixParts{P.part, P.ml, P.nsplit, P.rows};
+    return st;
+}
+
+}  // namespace raas
+
 extern "C" {
 
 raas_status raas_create_weight_cache(const raas_weight_config* cfg, void* stream, raas_weight_cache** out) {
@@ -382,25 +316,17 @@ raas_status raas_weight_step(raas_weight_cache* c, int32_t layer, const void* q,
     if (!q || !k_new || !v_new || !out) return fail(RAAS_E_INVALID, "q, k_new, v_new and out must be non-NULL");
     if (!c->prefilled[layer]) return fail(RAAS_E_STATE, "layer %d has not been prefilled", layer);
     if (prefix) {
-        const raas_prefix_config& f = prefix->cfg;
-        if (f.n_q_heads != c->cfg.n_q_heads || f.n_kv_heads != c->cfg.n_kv_heads || f.head_dim != c->cfg.head_dim ||
-            f.dtype != c->cfg.dtype)
-            return fail(RAAS_E_INVALID, "the prefix has other heads or another type than the cache");
-        if (prefix->device != c->device) return fail(RAAS_E_INVALID, "the prefix lies on another device");
-        if (layer >= f.n_layers) return fail(RAAS_E_INVALID, "the prefix has no layer %d", layer);
-        if (prefix->stored[layer] < 0) return fail(RAAS_E_STATE, "layer %d of the prefix has not been stored", layer);
-        if (c->cfg.batch > f.max_rows)
-            return fail(RAAS_E_INVALID, "batch %d exceeds the prefix's max_rows %d", c->cfg.batch, f.max_rows);
+        st = check_step_prefix(prefix, layer,
+                               {c->cfg.n_q_heads, c->cfg.n_kv_heads, c->cfg.head_dim, c->cfg.dtype, c->device, c->cfg.batch});
+        if (st != RAAS_OK) return st;
     }
     DeviceScope scope(c->device);
     if (scope.error() != hipSuccess) return hip_fail(scope.error(), "hipSetDevice");
     hipStream_t s = (hipStream_t)stream;
     WeightStepIO io{q, k_new, v_new, out, positions_out, weights_out, evicted_out, active, PrefixParts{}};
     if (prefix) {
-        PrefixView P;
-        st = prefix_parts(prefix, layer, q, c->cfg.batch, P, s);
+        st = step_prefix_parts(prefix, layer, q, c->cfg.batch, io.prefix, s);
         if (st != RAAS_OK) return st;
-        io.prefix = PrefixParts{P.part, P.ml, P.nsplit, P.rows};
     }
     // What other layers, caches and pools have read since the layer's last step
     // decides whether it is still in the memory-side cache; a captured step, whose

@@ -1,0 +1,726 @@
+"""The quantised cache: refusals without a GPU, and on the GPU what it holds and
+its attention against their fp64 statements (tests/quant_reference.py)."""
+from __future__ import annotations
+
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+import quant_reference as ref
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "raas.h")
+BITS = [(4, 4), (8, 8), (8, 4), (4, 8)]
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2502_11147_amd as raas
+
+    if not os.path.exists(raas.LIB_PATH):
+        from paper_2502_11147_amd import build as b
+
+        b.build()
+    return raas.load_library()
+
+
+@pytest.fixture(autouse=True)
+def _needs_gpu(request):
+    if request.node.get_closest_marker("gpu") is None:
+        return
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+# ---------------------------------------------------------------------------
+# Without a GPU.
+
+def _config(**kw):
+    import paper_2502_11147_amd as raas
+
+    base = dict(n_layers=2, n_q_heads=8, n_kv_heads=2, head_dim=128, page_size=64, n_pages=10, max_batch=3, max_queries=4,
+                key_bits=4, value_bits=8, dtype=raas.BF16)
+    base.update(kw)
+    return raas.QuantConfig(**base)
+
+
+BAD = [dict(n_layers=0), dict(n_layers=-1), dict(n_q_heads=7), dict(n_q_heads=0), dict(n_q_heads=34), dict(n_kv_heads=0),
+       dict(n_q_heads=65536, n_kv_heads=65536), dict(head_dim=96), dict(page_size=0), dict(page_size=16),
+       dict(page_size=96), dict(page_size=512), dict(page_size=-32), dict(n_pages=0), dict(n_pages=-5), dict(max_batch=0),
+       dict(max_batch=4097), dict(max_queries=0), dict(max_queries=1 << 23), dict(max_queries=2 ** 31 - 1),
+       dict(key_bits=3), dict(key_bits=0), dict(value_bits=16), dict(value_bits=-4), dict(dtype=2), dict(dtype=-1)]
+
+
+@pytest.mark.parametrize("bad", BAD, ids=lambda b: ",".join("%s=%s" % kv for kv in b.items()))
+def test_create_refuses(lib, bad):
+    import paper_2502_11147_amd as raas
+
+    h = ctypes.c_void_p()
+    assert lib.raas_create_quant_cache(ctypes.byref(_config(**bad)), None, ctypes.byref(h)) == raas.E_INVALID
+    assert not h.value and lib.raas_last_error()
+
+
+@pytest.mark.parametrize("sizes", [dict(n_layers=2 ** 31 - 1, n_pages=2 ** 31 - 1),
+                                   dict(n_layers=1 << 20, n_pages=1 << 30, n_kv_heads=1, page_size=256)])
+def test_create_of_more_bytes_than_64_bits_count(lib, sizes):
+    import paper_2502_11147_amd as raas
+
+    h = ctypes.c_void_p()
+    assert lib.raas_create_quant_cache(ctypes.byref(_config(**sizes)), None, ctypes.byref(h)) == raas.E_OOM
+    assert not h.value and b"bytes" in lib.raas_last_error()
+
+
+def test_null_handles(lib):
+    import paper_2502_11147_amd as raas
+
+    cfg = _config()
+    assert lib.raas_create_quant_cache(ctypes.byref(cfg), None, None) == raas.E_INVALID
+    h = ctypes.c_void_p()
+    assert lib.raas_create_quant_cache(None, None, ctypes.byref(h)) == raas.E_INVALID
+    for call in (lib.raas_quant_write, lib.raas_quant_read):
+        assert call(None, 0, 64, 64, 64, 1, 64, None, 1, 1, None) == raas.E_INVALID
+    assert lib.raas_quant_attention(None, 0, 64, 64, 1, 64, None, 1, 1, 64, None, None) == raas.E_INVALID
+    assert lib.raas_quant_step(None, 0, 64, 64, 64, 64, 1, 64, 1, 64, None, None, None, None, None) == raas.E_INVALID
+    lib.raas_destroy_quant_cache(None)
+    assert lib.raas_quant_cache_bytes(None) == 0
+
+
+def test_config_layout_matches_header():
+    import paper_2502_11147_amd as raas
+
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    body = text[text.rindex("typedef struct {", 0, text.index("} raas_quant_config;")):]
+    fields = re.findall(r"int32_t\s+(\w+);", body[:body.index("}")])
+    assert fields == [n for n, _ in raas.QuantConfig._fields_]
+
+
+def test_reference_holds_what_the_format_says():
+    """The reference's own corners: the limit of a group's maximum, ties, signs, zeros."""
+    x = np.zeros(32)
+    x[:8] = [6.999, 0.25, 0.75, -1.25, 2.5, 5.0, -0.2, 3.5]
+    assert np.array_equal(ref.held(x, 4)[:8], [6, 0, 1, -1, 2, 4, -0.0, 4])
+    x[0] = 7.0  # the next power of two: steps of 1 from 0 on
+    assert np.array_equal(ref.held(x, 4)[:8], [8, 0, 1, -1, 2, 4, -0.0, 4])
+    x[0] = 463.0
+    assert ref.held(x, 8)[0] == 448 and ref.held(x * 2, 8)[0] == 896
+    x[0] = 464.0
+    assert ref.held(x, 8)[0] == 448  # at twice the power 232, half way between 224 (even) and 240
+    assert not ref.held(np.zeros(32), 4).any()
+    x[1] = np.inf
+    assert np.isnan(ref.held(x, 8)).all()
+
+
+# ---------------------------------------------------------------------------
+# On the GPU.
+
+def _dtype(name):
+    import torch
+
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _dev(a, dtype, offset=0):
+    """The array as a device tensor, `offset` elements into its memory."""
+    import torch
+
+    a = np.asarray(a)
+    mem = torch.zeros(a.size + offset, dtype=dtype, device="cuda")
+    t = mem[offset:].view(a.shape)
+    t.copy_(torch.from_numpy(np.ascontiguousarray(a)).to(dtype))
+    return t
+
+
+def _ints(a):
+    import torch
+
+    return _dev(np.asarray(a, np.int64), torch.int32)
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _same(got, want, what=""):
+    assert np.array_equal(got, want, equal_nan=True), (what, np.argwhere(~((got == want) | (np.isnan(got) & np.isnan(want))))[:5])
+
+
+def _within(got, want, bound, what):
+    inf = np.isneginf(want)
+    assert np.array_equal(np.isneginf(got), inf), what
+    got, want = np.where(inf, 0, got), np.where(inf, 0, want)
+    assert np.isfinite(got).all(), what
+    over = np.abs(got - want) - bound
+    at = np.unravel_index(np.argmax(over), over.shape)
+    assert over[at] <= 0, (what, at, got[at], want[at], bound[at])
+
+
+class Model:
+    """A cache of `layers` layers beside what it should hold: K, V per sequence [Hkv][tokens][d] in fp64."""
+
+    def __init__(self, lens, hq, hkv, d, bits=(4, 4), dtype="bf16", page=32, spare=3, room=64, max_queries=1, layer=0,
+                 layers=1, seed=0, offset=0, width=None):
+        import paper_2502_11147_amd as raas
+
+        self.rng = np.random.default_rng(seed)
+        self.B, self.hq, self.hkv, self.d, self.bits, self.dt, self.page = len(lens), hq, hkv, d, bits, _dtype(dtype), page
+        self.bf16, self.layer, self.offset = dtype == "bf16", layer, offset
+        self.width = width or -(-(max(list(lens) + [0]) + room) // page)
+        n = self.B * self.width + spare
+        self.cache = raas.QuantCache(layers, hq, hkv, d, n_pages=n, page_size=page, max_batch=self.B, max_queries=max_queries,
+                                     key_bits=bits[0], value_bits=bits[1], dtype=dtype)
+        self.pages = self.rng.permutation(n)[:self.B * self.width].reshape(self.B, self.width)
+        self.table = _ints(self.pages)
+        self.K = [np.zeros((hkv, 0, d)) for _ in lens]
+        self.V = [np.zeros((hkv, 0, d)) for _ in lens]
+        if max(list(lens) + [0]) > 0:
+            self.write(lens)
+
+    def data(self, *shape):
+        x = self.rng.standard_normal(shape).astype(np.float32)
+        x[..., ::29] *= 5
+        t = _dev(x, self.dt, self.offset)
+        return t, _np(t)
+
+    def lens(self):
+        return [k.shape[1] for k in self.K]
+
+    def write(self, counts, rows=None):
+        """counts[b] new tokens behind what sequence b holds."""
+        n = rows or max(max(counts), 1)
+        (k, kn), (v, vn) = self.data(self.B, self.hkv, n, self.d), self.data(self.B, self.hkv, n, self.d)
+        self.cache.write(self.layer, k, v, self.table, _ints(self.lens()), _ints(counts))
+        for b, c in enumerate(counts):
+            if c > 0:
+                self.K[b] = np.concatenate([self.K[b], ref.held(kn[b, :, :c], self.bits[0])], 1)
+                self.V[b] = np.concatenate([self.V[b], ref.held(vn[b, :, :c], self.bits[1])], 1)
+
+    def check_held(self, lens=None):
+        import torch
+
+        lens = lens or self.lens()
+        n = max(max(lens), 1)
+        k, v = (torch.full((self.B, self.hkv, n, self.d), -7.0, dtype=self.dt, device="cuda") for _ in range(2))
+        self.cache.read(self.layer, k, v, self.table, _ints([0] * self.B), _ints(lens))
+        for name, got, want in (("k", _np(k), self.K), ("v", _np(v), self.V)):
+            for b in range(self.B):
+                _same(got[b, :, :lens[b]], want[b][:, :lens[b]], (name, b))
+                assert (got[b, :, lens[b]:] == -7.0).all()
+
+    def query(self, *lead):
+        """Queries that lean towards keys, so that weights concentrate."""
+        q = self.rng.standard_normal(lead + (self.hq, self.d)) * 1.5
+        t = _dev(q.astype(np.float32), self.dt, self.offset)
+        return t, _np(t)
+
+    def attend(self, n, counts=None, lens=None, seen=None):
+        """seen(b, tokens): which of the held tokens count (None: all)."""
+        import torch
+
+        lens = lens or self.lens()
+        q, qn = self.query(self.B, n)
+        out = torch.full(q.shape, 9.0, dtype=self.dt, device="cuda")
+        lse = torch.full(q.shape[:3], 9.0, dtype=torch.float32, device="cuda")
+        self.cache.attend(self.layer, q, out, self.table, _ints(lens), None if counts is None else _ints(counts), lse)
+        got, gl, G = _np(out), _np(lse), self.hq // self.hkv
+        for b in range(self.B):
+            c = n if counts is None else min(max(counts[b], 0), n)
+            if lens[b] < 0:
+                c = 0
+            assert (got[b, c:] == 9.0).all() and (gl[b, c:] == 9.0).all(), b
+            for i in range(c):
+                last = max(0, min(lens[b], self.width * self.page) - c + i + 1)
+                for h in range(self.hkv):
+                    K, V = self.K[b][h, :last], self.V[b][h, :last]
+                    if seen is not None:
+                        K, V = K[seen(b, last)], V[seen(b, last)]
+                    heads = slice(h * G, (h + 1) * G)
+                    o, ob, l, lb = ref.attention(qn[b, i, heads], K, V, self.bf16)
+                    _within(got[b, i, heads], o, ob, ("out", b, i, h))
+                    _within(gl[b, i, heads], l, lb, ("lse", b, i, h))
+        return out, lse
+
+    def step(self, active=None, prefix=None, check=True):
+        import torch
+
+        B, G = self.B, self.hq // self.hkv
+        lens = [n if active is None or active[b] else -1 - b for b, n in enumerate(self.lens())]
+        q, qn = self.query(B)
+        (k, kn), (v, vn) = self.data(B, self.hkv, self.d), self.data(B, self.hkv, self.d)
+        full = lambda *s, dt=self.dt: torch.full(s, 9.0, dtype=dt, device="cuda")
+        out, lse = full(B, self.hq, self.d), full(B, self.hq, dt=torch.float32)
+        kh, vh = full(B, self.hkv, self.d), full(B, self.hkv, self.d)
+        self.cache.decode_step(self.layer, q, k, v, out, self.table, _ints(lens), lse, kh, vh,
+                               prefix=None if prefix is None else prefix[0])
+        for b in range(B):
+            if lens[b] >= 0:
+                self.K[b] = np.concatenate([self.K[b], ref.held(kn[b], self.bits[0])[:, None]], 1)
+                self.V[b] = np.concatenate([self.V[b], ref.held(vn[b], self.bits[1])[:, None]], 1)
+        if not check:
+            return
+        got, gl, gk, gv = _np(out), _np(lse), _np(kh), _np(vh)
+        for b in range(B):
+            if lens[b] < 0:
+                for x in (got, gl, gk, gv):
+                    assert (x[b] == 9.0).all(), b
+                continue
+            _same(gk[b], self.K[b][:, -1])
+            _same(gv[b], self.V[b][:, -1])
+            for h in range(self.hkv):
+                heads = slice(h * G, (h + 1) * G)
+                o, ob, l, lb = ref.attention(qn[b, heads], self.K[b][h], self.V[b][h], self.bf16,
+                                             None if prefix is None else (prefix[1][h], prefix[2][h]))
+                _within(got[b, heads], o, ob, ("out", b, h))
+                _within(gl[b, heads], l, lb, ("lse", b, h))
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_held_values(dtype, bits, d):
+    """Magnitudes over the whole range, ties, zeros, groups at the limit of a power of two."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    rng = np.random.default_rng(d + bits[0])
+    n, hkv = 700, 2
+    c = raas.QuantCache(1, hkv, hkv, d, n_pages=30, page_size=32, max_batch=1, key_bits=bits[0], value_bits=bits[1], dtype=dtype)
+    table = _ints(rng.permutation(30)[None])
+    xs = []
+    for b in bits:
+        x = rng.standard_normal((1, hkv, n, d))
+        x[:, :, :200] *= 2.0 ** rng.integers(-100, 100, (1, hkv, 200, 1))
+        # ties and the limits: a group's maximum at each value of the grid and between, the others half way
+        grid = ref.values(b)
+        mid = np.concatenate([grid, (grid[1:] + grid[:-1]) / 2, [7.0 if b == 4 else 464.0, 6.97 if b == 4 else 463.0]])
+        for t in range(200, 600):
+            g = rng.choice(mid, d) * rng.choice([-1, 1], d)
+            g[::32] = rng.choice(mid[len(mid) // 2:], d // 32)
+            x[0, :, t] = g * 2.0 ** rng.integers(-20, 20)
+        x[0, :, 600:620] = 0
+        x[0, :, 620:640] *= 2.0 ** -110
+        x[0, :, 640:650] *= 2.0 ** -126
+        x[0, :, 650:660] = np.clip(x[0, :, 650:660], -1.9, 1.9) * 2.0 ** 127
+        xs.append(_dev(x.astype(np.float32), _dtype(dtype)))
+    c.write(0, *xs, table, _ints([0]))
+    out = [torch.empty_like(x) for x in xs]
+    c.read(0, *out, table, _ints([0]))
+    for x, o, b in zip(xs, out, bits):
+        _same(_np(o), ref.held(_np(x), b), b)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+def test_groups_with_nan(bits, d):
+    """Infinities and NaN make their own group NaN, no other."""
+    m = Model([0], 2, 2, d, bits, room=70)
+    import torch
+
+    x = m.rng.standard_normal((1, 2, 65, d)).astype(np.float32)
+    x[0, 0, 3, 5], x[0, 1, 31, 40], x[0, 0, 64, 63], x[0, 1, 33, 0] = np.nan, np.inf, -np.inf, -np.nan
+    k, v = _dev(x, m.dt), _dev(x[:, ::-1], m.dt)
+    m.cache.write(0, k, v, m.table, _ints([0]))
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    m.cache.read(0, ko, vo, m.table, _ints([0]))
+    _same(_np(ko), ref.held(_np(k), bits[0]))
+    _same(_np(vo), ref.held(_np(v), bits[1]))
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_written_in_pieces(dtype, bits, d, offset):
+    """Ragged pieces that start and end anywhere in a block; what lies around them stays."""
+    m = Model([0, 0, 0, 0], 4, 2, d, bits, dtype, room=200, layers=2, layer=1, offset=offset)
+    for counts in ([5, 0, 32, 33], [1, 1, 1, 1], [26, 64, 40, -3], [33, 95, 0, 60]):
+        m.write(counts, rows=96)
+        m.check_held()
+    # a part of the tokens, from an odd one on
+    import torch
+
+    k, v = (torch.full((4, 2, 40, d), 3.0, dtype=m.dt, device="cuda") for _ in range(2))
+    m.cache.read(1, k, v, m.table, _ints([7, 31, 0, -1]), _ints([40, 99, 0, 5]))
+    got = _np(k)
+    for b, (s, c) in enumerate([(7, 40), (31, 40), (0, 0), (0, 0)]):
+        _same(got[b, :, :c], m.K[b][:, s:s + c])
+        assert (got[b, :, c:] == 3.0).all()
+
+
+SHAPES = [(1, 1, 64), (8, 2, 64), (7, 1, 128), (32, 2, 128), (6, 3, 128)]
+
+
+@gpu
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_one_query(dtype, bits, shape):
+    m = Model([0, 1, 31, 32, 33, 300, 64], *shape, bits, dtype, page=64)
+    m.attend(1)
+    m.attend(1, counts=[1, 1, 0, 1, -1, 1, 5], lens=[0, 0, 31, 30, 33, 299, -1])
+
+
+@gpu
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("queries", [2, 3, 5, 9, 16, 40, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_several_queries(dtype, queries, shape):
+    """Every row tile; counts below the rows, above the tokens held, none."""
+    bits = BITS[queries % 4]
+    m = Model([300, 33, 7, 0, queries], *shape, bits, dtype, page=32, max_queries=70, offset=1)
+    m.attend(queries)
+    m.attend(queries, counts=[queries - 1, 1, queries, queries, 0])
+
+
+@gpu
+@pytest.mark.parametrize("shape,dtype", [((32, 8, 128), "bf16"), ((14, 2, 64), "bf16"), ((4, 2, 128), "f32"), ((16, 1, 64), "f32")],
+                         ids=str)
+@pytest.mark.parametrize("bits", BITS, ids=str)
+def test_steps(shape, dtype, bits):
+    """From empty sequences over blocks and pages, some sitting out."""
+    m = Model([0, 30, 63], *shape, bits, dtype, page=32, room=80, layers=2, layer=1, offset=1)
+    for t in range(70):
+        m.step(active=None if t % 3 else [t % 2, 1, 0], check=t < 6 or t % 16 == 0)
+    m.check_held()
+    m.step()
+
+
+@gpu
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f32")])
+def test_steps_behind_a_prefix(d, dtype):
+    import paper_2502_11147_amd as raas
+
+    m = Model([0, 400, 3], 8, 2, d, (8, 4), dtype, page=64)
+    for tokens in (0, 1, 700):
+        p = raas.SharedPrefix(1, 8, 2, d, 700, 3, dtype)
+        (k, kn), (v, vn) = m.data(2, max(tokens, 1), d), m.data(2, max(tokens, 1), d)
+        p.store(0, k if tokens else None, v if tokens else None)
+        for t in range(3):
+            m.step(active=[1, 1, t], prefix=(p, kn[:, :tokens], vn[:, :tokens]))
+
+
+@gpu
+@pytest.mark.parametrize("lens", [[20000], [9000, 1, 0, 40, 70, 3000], [5] * 70 + [2500] + [33] * 64, [1] * 130], ids=lambda l: "%d-%d" % (len(l), max(l)))
+def test_ragged_batches(lens):
+    """Long sequences beside short ones, more sequences than lanes: units over many workgroups."""
+    m = Model(lens, 4, 1, 64, (4, 8), page=128, max_queries=3)
+    m.attend(1)
+    m.step(active=[b % 5 != 1 for b in range(len(lens))])
+    m.attend(3, counts=[b % 4 for b in range(len(lens))])
+
+
+@gpu
+def test_one_sequence_of_many_heads():
+    m = Model([3000], 32, 8, 128, (4, 4), page=256, max_queries=8)
+    m.attend(1)
+    m.step()
+    m.attend(8)
+
+
+@gpu
+@pytest.mark.parametrize("bits", BITS, ids=str)
+def test_stale_memory_is_not_seen(bits):
+    """Every page held NaN before: what lies behind a sequence's last token does not matter."""
+    import torch
+
+    for d in (64, 128):
+        m = Model([0, 0, 0], 4, 2, d, bits, page=64, room=130, max_queries=4, spare=0)
+        bad = torch.full((3, 2, m.width * 64, d), float("nan"), dtype=m.dt, device="cuda")
+        m.cache.write(0, bad, bad, m.table, _ints([0, 0, 0]))
+        m.write([1, 37, 95])
+        m.attend(1)
+        m.attend(4)
+        m.step()
+        m.step(active=[1, 0, 1])
+
+
+@gpu
+def test_entries_that_are_no_page():
+    """Their tokens are neither written, read nor attended to, and nothing else is touched."""
+    import torch
+
+    m = Model([200, 200, 200, 200], 8, 2, 128, (4, 8), page=32, max_queries=3, spare=0)
+    n = m.cache.n_pages
+    m.pages[0, 2], m.pages[1, 0], m.pages[2, :], m.pages[3, 6] = -1, n, -5, 2 ** 31 - 1
+    m.table = _ints(m.pages)
+    good = [np.repeat((m.pages[b] >= 0) & (m.pages[b] < n), 32) for b in range(4)]
+    seen = lambda b, last: good[b][:last]
+    m.attend(1, seen=seen)
+    m.attend(3, seen=seen)
+    k, v = (torch.full((4, 2, 200, 128), 3.0, dtype=m.dt, device="cuda") for _ in range(2))
+    m.cache.read(0, k, v, m.table, _ints([0] * 4))
+    got = _np(v)
+    for b in range(4):
+        _same(got[b][:, good[b][:200]], m.V[b][:, good[b][:200]])
+        assert (got[b][:, ~good[b][:200]] == 3.0).all()
+    m.cache.write(0, k * 0, v * 0, m.table, _ints([0, 0, 0, 192]), _ints([0, 32, 200, 8]))  # no page: stores nothing
+    m.attend(3, seen=seen)
+    # a step whose new token finds no page attends to the others
+    q, qn = m.query(4)
+    out, held = torch.full(q.shape, 9.0, dtype=m.dt, device="cuda"), torch.full((4, 2, 128), 9.0, dtype=m.dt, device="cuda")
+    m.cache.decode_step(0, q, v[:, :, 0].contiguous(), v[:, :, 0].contiguous(), out, m.table, _ints([-1, -1, 200, 199]), None, held)
+    assert (_np(held) == 9.0).all() and not _np(out)[2].any()
+    for h in range(2):
+        o, ob, _, _ = ref.attention(qn[3, 4 * h:4 * h + 4], m.K[3][h, :192], m.V[3][h, :192], True)
+        _within(_np(out)[3, 4 * h:4 * h + 4], o, ob, h)
+
+
+@gpu
+def test_lengths_past_the_table():
+    """Tokens past the table's row are not stored; lengths past it count as its end."""
+    m = Model([0, 60], 4, 1, 64, (8, 8), page=32, width=2, max_queries=2)
+    m.write([64, 4])
+    big = _dev(np.ones((2, 1, 3, 64), np.float32), m.dt)
+    m.cache.write(0, big, big, m.table, _ints([64, 2 ** 31 - 1]))  # nowhere
+    m.check_held()
+    m.attend(1, lens=[64, 2 ** 31 - 1])
+    m.attend(2, lens=[1 << 20, 64])
+    import torch
+
+    q, _ = m.query(2)
+    out, held = torch.empty_like(q), torch.full((2, 1, 64), 9.0, dtype=m.dt, device="cuda")
+    m.cache.decode_step(0, q, big[:, :, 0].contiguous(), big[:, :, 0].contiguous(), out, m.table, _ints([64, 1 << 30]), None, held)
+    assert (_np(held) == 9.0).all()
+    m.check_held()
+
+
+@gpu
+def test_shared_pages():
+    """Two sequences behind the same first page, which neither writes."""
+    m = Model([64, 64], 4, 2, 128, page=64)
+    m.pages[1, 0] = m.pages[0, 0]
+    m.table = _ints(m.pages)
+    m.K[1], m.V[1] = m.K[0].copy(), m.V[0].copy()
+    m.attend(1)
+    m.step()
+    m.write([3, 40])
+    m.check_held()
+    m.attend(1)
+
+
+@gpu
+def test_offsets_past_32_bits():
+    """A pool of 9 GB: pages at its far end."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    n = 140000
+    c = raas.QuantCache(1, 4, 4, 128, n_pages=n, page_size=64, max_batch=1, key_bits=8, value_bits=8)
+    assert c.device_bytes() > 2 ** 33
+    m = Model([0], 4, 4, 128, (8, 8), page=64, room=300)
+    m.cache = c
+    m.pages = np.array([[n - 1, 0, n // 2, n - 2, 63551, 63552]])
+    m.width = 6
+    m.table = _ints(m.pages)
+    m.write([300])
+    m.check_held()
+    m.attend(1)
+    m.step()
+    del torch
+
+
+@gpu
+def test_same_bits():
+    """The same calls on the same contents."""
+    m = Model([7000, 33, 500], 8, 2, 128, (4, 4), page=64, max_queries=5)
+    import torch
+
+    q, _ = m.query(3, 5)
+    outs = []
+    for _ in range(4):
+        out, lse = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")
+        m.cache.attend(0, q, out, m.table, _ints(m.lens()), None, lse)
+        outs.append((out, lse))
+    for o, l in outs[1:]:
+        assert torch.equal(o, outs[0][0]) and torch.equal(l, outs[0][1])
+
+
+@gpu
+def test_captured_and_replayed():
+    """A captured write, attention and step follow the lengths, the table and the inputs
+    that hold when they run; eager work in between."""
+    import torch
+
+    m = Model([100, 5, 0], 8, 2, 64, (4, 8), page=32, max_queries=2, room=100)
+    B, w = 3, m.width
+    lens, table = _ints(m.lens()), m.table.clone()
+    q = m.query(B, 2)[0]
+    q1 = q[:, 0].contiguous()
+    k, v = (m.data(B, 2, 2, 64)[0] for _ in range(2))
+    kn, vn = (m.data(B, 2, 64)[0] for _ in range(2))
+    one = torch.ones(B, dtype=torch.int32, device="cuda")
+    outs = [torch.zeros_like(q), torch.zeros_like(q1), torch.zeros_like(kn)]
+
+    def calls(o):
+        m.cache.write(0, k, v, table, lens)
+        m.cache.attend(0, q, o[0], table, lens + 2 * one)
+        m.cache.decode_step(0, q1, kn, vn, o[1], table, lens + 2 * one, k_held=o[2])
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        calls(outs)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls(outs)
+    for t in range(4):
+        lens.copy_(_ints([100 + 9 * t, 40 * t, 31 + t]))
+        table.copy_(m.table if t % 2 == 0 else m.table.flip(1))
+        for x in (q, q1, k, v, kn, vn):
+            x.copy_(torch.randn(x.shape, device="cuda"))
+        torch.cuda.synchronize()
+        g.replay()
+        got = [o.clone() for o in outs]
+        torch.cuda.synchronize()
+        want = [torch.zeros_like(o) for o in outs]
+        calls(want)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y), t
+
+
+@gpu
+def test_other_streams():
+    """Calls on a stream of their own, and two caches at once on two streams."""
+    import torch
+
+    ms = [Model([600, 2000], 8, 2, 128, BITS[i], page=64, max_queries=2, seed=i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ms]
+    qs = [m.query(2, 2)[0] for m in ms]
+    lens = [_ints(m.lens()) for m in ms]
+    want = []
+    for m, q, l in zip(ms, qs, lens):
+        o = torch.zeros_like(q)
+        m.cache.attend(0, q, o, m.table, l)
+        want.append(o)
+    got = [torch.zeros_like(q) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for m, q, l, o, s in zip(ms, qs, lens, got, streams):
+            m.cache.attend(0, q, o, m.table, l, stream=s)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
+@gpu
+def test_call_refusals(lib):
+    """Arguments out of range change nothing and launch nothing."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    m = Model([40, 3], 8, 2, 128, (4, 4), page=32, max_queries=2)
+    h, t = m.cache.handle, m.table
+    lens = _ints([40, 3])
+    q = torch.zeros(2, 2, 8, 128, dtype=m.dt, device="cuda")
+    kv = torch.zeros(2, 2, 1, 128, dtype=m.dt, device="cuda")
+    p = lambda x: x.data_ptr()
+
+    def write(layer=0, k=p(kv), v=p(kv), table=p(t), width=m.width, start=p(lens), batch=2, tokens=1, call="write"):
+        return getattr(lib, "raas_quant_" + call)(h, layer, k, v, table, width, start, None, batch, tokens, None)
+
+    def attend(layer=0, q_=p(q), table=p(t), width=m.width, l=p(lens), batch=2, n=2, out=p(q)):
+        return lib.raas_quant_attention(h, layer, q_, table, width, l, None, batch, n, out, None, None)
+
+    def step(layer=0, q_=p(q), k=p(kv), v=p(kv), table=p(t), width=m.width, l=p(lens), batch=2, out=p(q), prefix=None):
+        return lib.raas_quant_step(h, layer, q_, k, v, table, width, l, batch, out, None, None, None, prefix, None)
+
+    shared = [dict(layer=-1), dict(layer=1), dict(table=None), dict(width=0), dict(width=-1), dict(width=(1 << 20) // 32 + 1),
+              dict(batch=-1), dict(batch=3)]
+    for kw in shared + [dict(k=None), dict(v=None), dict(start=None), dict(tokens=-1), dict(tokens=(1 << 20) + 1)]:
+        assert write(**kw) == raas.E_INVALID and write(call="read", **kw) == raas.E_INVALID, kw
+    for kw in shared + [dict(q_=None), dict(l=None), dict(out=None), dict(n=-1), dict(n=3)]:
+        assert attend(**kw) == raas.E_INVALID, kw
+    for kw in shared + [dict(q_=None), dict(k=None), dict(v=None), dict(l=None), dict(out=None)]:
+        assert step(**kw) == raas.E_INVALID, kw
+    assert write(batch=0, table=None) == raas.OK and write(tokens=0, k=None) == raas.OK
+    assert attend(batch=0, table=None) == raas.OK and attend(n=0, q_=None) == raas.OK and step(batch=0, q_=None) == raas.OK
+    prefix = raas.SharedPrefix(1, 8, 2, 128, 64, 1)
+    assert step(prefix=prefix.handle) == raas.E_STATE  # not stored
+    prefix.store(0, None, None)
+    assert step(prefix=prefix.handle) == raas.E_INVALID  # of one row
+    for other in (raas.SharedPrefix(1, 4, 2, 128, 64, 2), raas.SharedPrefix(1, 8, 2, 64, 64, 2), raas.SharedPrefix(1, 8, 2, 128, 64, 2, "f32")):
+        assert step(prefix=other.handle) == raas.E_INVALID
+    torch.cuda.synchronize()
+    m.check_held()
+    c = m.cache
+    k4 = kv
+    with pytest.raises(TypeError):
+        c.write(0, k4.cpu(), k4.cpu(), t, lens)
+    with pytest.raises(TypeError):
+        c.write(0, k4[0], k4[0], t, lens)
+    with pytest.raises(ValueError):
+        c.write(0, k4, k4, t, lens[:1])
+    with pytest.raises(ValueError):
+        c.write(0, k4, k4.float(), t, lens)
+    with pytest.raises(TypeError):
+        c.write(0, k4, k4, t, None)
+    with pytest.raises(ValueError):
+        c.write(0, k4, k4, t.long(), lens)
+    with pytest.raises(ValueError):
+        c.attend(0, q, q, t[:, ::2], lens)
+    with pytest.raises(ValueError):
+        c.attend(0, q, q[:, :1], t, lens)
+    with pytest.raises(TypeError):
+        c.decode_step(0, q[:, 0].contiguous(), kv[:, :, 0], kv[:, :, 0], q[:, 0].contiguous(), t, lens, prefix=3)
+    with pytest.raises(TypeError):
+        c.decode_step(0, q, kv, kv, q, t, lens)
+    s = c.prepare_step(0, q[:, 0].contiguous(), kv[:, :, 0].contiguous(), kv[:, :, 0].contiguous(), q[:, 0].contiguous(), t, lens,
+                       prefix=prefix)
+    prefix.close()
+    with pytest.raises(ValueError):
+        c.decode_prepared(s)
+    c.close()
+    with pytest.raises(raas.RaasError):
+        c.write(0, k4, k4, t, lens)
+
+
+@gpu
+def test_created_on_a_capturing_stream(lib):
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    x = torch.zeros(4, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        x += 1
+        with pytest.raises(raas.RaasError) as e:
+            raas.QuantCache(1, 4, 2, 64, n_pages=4)
+        assert e.value.code == raas.E_STATE
+    g.replay()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_together(dtype):
+    """Requests as a server runs them: a prompt in two pieces with their attention, steps, a
+    draft of three tokens of which one stays, a request that ends and another in its pages,
+    held tokens read back."""
+    m = Model([0, 0, 0], 8, 2, 128, (8, 4), dtype, page=32, room=300, max_queries=90, offset=1)
+    m.write([90, 40, 0])
+    m.attend(90, counts=[90, 40, 0])
+    m.write([0, 55, 70])
+    m.attend(70, counts=[0, 55, 70])
+    for t in range(4):
+        m.step(active=[1, 1, t % 2])
+    m.write([3, 3, 3])
+    m.attend(3)
+    for b in range(3):  # two of the three are refused
+        m.K[b], m.V[b] = m.K[b][:, :-2], m.V[b][:, :-2]
+    m.step()
+    m.K[1], m.V[1] = m.K[1][:, :0], m.V[1][:, :0]
+    m.write([0, 20, 0])
+    m.attend(20, counts=[0, 20, 0])
+    m.step()
+    m.check_held()
