@@ -108,6 +108,21 @@ __device__ __forceinline__ int blocks_of(const QuantView& L, const QuantAttentio
     return blocks_of(held + (io.k_new != nullptr && held < L.cap ? 1 : 0));
 }
 
+// Sum over this lane and those before it: within rows of 16 lanes by 1, 2, 4 and 8
+// places, then the last lane of a row, and of the lower half, onto those behind.
+__device__ __forceinline__ int scan_sum(int x) {
+    auto add = [&](auto ctrl, auto rows) {
+        x += __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    };
+    add(Int<0x111>(), Int<0xF>());
+    add(Int<0x112>(), Int<0xF>());
+    add(Int<0x114>(), Int<0xF>());
+    add(Int<0x118>(), Int<0xF>());
+    add(Int<0x142>(), Int<0xA>());
+    add(Int<0x143>(), Int<0xC>());
+    return x;
+}
+
 // The workgroup's work, or false where there is less than the grid allows for.
 template <int ROWS>
 __device__ __forceinline__ bool find_work(const QuantView& L, const QuantAttention& io, const Cut& cut, int lane, int wg,
@@ -131,18 +146,12 @@ __device__ __forceinline__ bool find_work(const QuantView& L, const QuantAttenti
         const int parts = parts_of(blocks_of(L, io, t0)), n = r0 > 0 ? L.nkv * tiles_of(r0) * parts : 0;
         int upto = n, split = parts > 1 ? n : 0;
         const int own = split;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(upto, d), y = __shfl_up(split, d);
-            if (lane >= d) {
-                upto += x;
-                split += y;
-            }
-        }
+        upto = scan_sum(upto);
+        split = scan_sum(split);
         const unsigned long long m = __ballot(wg < before + upto);
         if (m == 0ull) {
-            before += __shfl(upto, 63);
-            slots += __shfl(split, 63);
+            before += __builtin_amdgcn_readlane(upto, 63);
+            slots += __builtin_amdgcn_readlane(split, 63);
             continue;
         }
         const int at = __ffsll(m) - 1;
@@ -382,10 +391,12 @@ __device__ __forceinline__ void take_token(const QuantAttention& io, Block<D, KB
 // and write the outputs, or publish the part: the last of a tile's parts to end
 // joins them all. Pages of a wavefront's next 64 blocks lie in its lanes.
 constexpr int kStreamWaves = 4;
-constexpr Cut kStreamCut = {1024, 2 * kStreamWaves};
+template <typename T, int RT>
+constexpr int kStreamPerSimd = sizeof(T) == 4 ? 1 : RT == 1 ? 3 : 2;
+constexpr Cut kStreamCut = {768, 2 * kStreamWaves};
 
 template <typename T, int D, int KB, int VB, int RT>
-__global__ __launch_bounds__(kStreamWaves * 64) void k_quant_stream(QuantView L, QuantAttention io) {
+__global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, RT>))) void k_quant_stream(QuantView L, QuantAttention io) {
     using F = Format<D, KB, VB>;
     constexpr int NW = kStreamWaves, TR = 16 * RT;
     __shared__ __align__(16) float s_o[NW][16][D + 4];
@@ -418,35 +429,46 @@ __global__ __launch_bounds__(kStreamWaves * 64) void k_quant_stream(QuantView L,
         const int b = lo + wv + (turn + lane) * NW;
         win = b < hi ? table[b >> L.page_shift] : -1;
     };
+    // This wavefront's blocks. The sequence's last one, if it is here, comes last, and
+    // only it takes a new token or ends with places that hold none.
+    const int turns = lo + wv < hi ? (hi - lo - wv + NW - 1) / NW : 0;
     Block<D, KB, VB> b0, b1;
     // page of the turn's block, -1: none; the block (of no page: any, unused)
     auto fetch = [&](int turn, Block<D, KB, VB>& blk) {
         if ((turn & 63) == 0) window(turn);
         int page = __builtin_amdgcn_readlane(win, turn & 63);
         page = page >= 0 && page < L.n_pages ? page : -1;
-        const int b = min(lo + wv + turn * NW, max(hi - 1, 0));
-        blk.load(record<F>(L, max(page, 0), b, w.h), lane);
+        blk.load(record<F>(L, max(page, 0), lo + wv + turn * NW, w.h), lane);
         return page;
     };
-    auto process = [&](int turn, int page, Block<D, KB, VB>& blk) {
-        if (page < 0) return;
-        const int b = lo + wv + turn * NW, t0 = b * kQuantBlock;
-        if (w.fresh >= t0 && w.fresh < t0 + kQuantBlock)
-            take_token<T, D, KB, VB>(io, blk, record<F>(L, page, b, w.h), w.fresh - t0, (size_t)w.b * L.nkv + w.h, lane);
-        if (t0 + kQuantBlock > w.tokens) blk.zero_values_from(w.tokens - t0, a);
+    auto attend = [&](int b, Block<D, KB, VB>& blk) {
+        const int t0 = b * kQuantBlock;
         int l[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) l[t] = lim[t] - t0;
         attend_block<T, D, KB, VB, RT>(blk, q, t0 + kQuantBlock > least, l, a, io.scale_log2, s);
     };
-    int p0 = fetch(0, b0);
-    for (int turn = 0; lo + wv + turn * NW < hi;) {
-        const int p1 = fetch(turn + 1, b1);
-        process(turn, p0, b0);
-        if (lo + wv + ++turn * NW >= hi) break;
-        p0 = fetch(turn + 1, b0);
-        process(turn, p1, b1);
-        ++turn;
+    if (turns > 0) {
+        int p0 = fetch(0, b0), turn = 0;
+        while (turn + 1 < turns) {
+            const int p1 = fetch(turn + 1, b1);
+            if (p0 >= 0) attend(lo + wv + turn * NW, b0);
+            if (++turn + 1 >= turns) {
+                b0 = b1;
+                p0 = p1;
+                break;
+            }
+            p0 = fetch(turn + 1, b0);
+            if (p1 >= 0) attend(lo + wv + turn * NW, b1);
+            ++turn;
+        }
+        if (p0 >= 0) {
+            const int b = lo + wv + turn * NW, t0 = b * kQuantBlock;
+            if (w.fresh >= t0 && w.fresh < t0 + kQuantBlock)
+                take_token<T, D, KB, VB>(io, b0, record<F>(L, p0, b, w.h), w.fresh - t0, (size_t)w.b * L.nkv + w.h, lane);
+            if (t0 + kQuantBlock > w.tokens) b0.zero_values_from(w.tokens - t0, a);
+            attend(b, b0);
+        }
     }
     const bool split = w.parts > 1;
 #pragma unroll
