@@ -20,7 +20,7 @@ KERNEL_PARTS = 15
 UNITS = [(KERNELS, ["-DRAAS_PART=%d" % i]) for i in range(KERNEL_PARTS)] + [
     (os.path.join(CSRC, name + ".hip"), [])
     for name in ("raas_weight_kernels", "raas_prefix_kernels", "raas_prompt_kernels", "raas_quant_kernels",
-                 "raas_quant_attention", "raas_runtime", "raas_weight_runtime", "raas_quant_runtime")]
+                 "raas_quant_attention", "raas_quant_wide", "raas_runtime", "raas_weight_runtime", "raas_quant_runtime")]
 # the streaming probe (measurement only) is a library of its own
 PROBE_SOURCES = [os.path.join(CSRC, "raas_probe.hip")]
 PROBE_LIB_PATH = os.path.join(HERE, "libraas_probe.so")

@@ -10,177 +10,12 @@
 
 #include <algorithm>
 
-#include "raas_quant_blocks.h"
+#include "raas_quant_attention.h"
 
 namespace raas {
 namespace {
 
 using namespace qnt;
-
-// ---------------------------------------------------------------------------
-// Eight fp32 numbers as the sum of N operands of the bf16 products. Each takes
-// the upper 16 bits of what is left, so three leave nothing of an fp32 number; the
-// second of two is rounded to bf16, which leaves at most 2^-15 of the number: less
-// than 2^-7 after the first, of which rounding is off by half a step, 2^-8. (One
-// bf16 alone would be off by 2^-8, as much as the rounding of a bf16 output.)
-template <int N>
-struct Pieces {
-    u32x4 p[N];
-    __device__ __forceinline__ Pieces() {}
-    __device__ __forceinline__ explicit Pieces(const float (&x)[8]) {
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = x[j];
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            if (N == 2 && n == 1) {
-                bf16x8 r;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) r[j] = (__bf16)y[j];
-                p[n] = __builtin_bit_cast(u32x4, r);
-                break;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)  // the upper halves of two side by side
-                p[n][j] = __builtin_amdgcn_perm(__float_as_uint(y[2 * j + 1]), __float_as_uint(y[2 * j]), 0x07060302u);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] -= __uint_as_float(__float_as_uint(y[j]) & 0xFFFF0000u);
-        }
-    }
-};
-// operands that a query, and a probability, of a cache of T is made of
-template <typename T>
-constexpr int kQueryPieces = sizeof(T) == 2 ? 1 : 3;
-template <typename T>
-constexpr int kProbPieces = sizeof(T) == 2 ? 2 : 3;
-
-__device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, f32x4 c) { return mfma16<uint16_t>(a, b, c); }
-
-// This lane's channels D/4 a + 8 ks .. of a query row.
-template <typename T, int D>
-__device__ __forceinline__ void load_query(const T* row, bool real, int a,
-                                           u32x4 (&q)[D / 32][kQueryPieces<T>]) {
-#pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) {
-        const T* at = row + a * (D / 4) + 8 * ks;
-        if constexpr (sizeof(T) == 2) {
-            q[ks][0] = real ? ld16_in<T>(at) : u32x4{0u, 0u, 0u, 0u};
-        } else {
-            float x[8] = {};
-            if (real) load_floats<T, 8>(at, x);
-            const Pieces<3> p(x);
-#pragma unroll
-            for (int n = 0; n < 3; ++n) q[ks][n] = p.p[n];
-        }
-    }
-}
-
-// ---------------------------------------------------------------------------
-// Which rows and blocks a workgroup takes. The rows of a unit (queries of its
-// sequence times G heads) are cut into tiles, a tile's tokens into parts of about
-// equally many blocks over the whole batch, so that ragged sequences load the
-// chip evenly: every workgroup finds its own from the lengths, which the host does
-// not know. Parts are cut so that about `target` workgroups come out, but of at
-// least `least` blocks, and at most kMaxQuantParts per tile.
-struct Cut {
-    int target, least;
-};
-struct Work {
-    int b, h, tile, tiles, part, parts;
-    int slot;    // of the tile's first part in the scratch, if parts > 1
-    int tokens;  // held by the sequence, a step's new one among them
-    int fresh;   // place of a step's new token, -1: none
-    int rows;    // of the unit
-};
-
-__device__ __forceinline__ int blocks_of(int tokens) { return (tokens + kQuantBlock - 1) / kQuantBlock; }
-// A sequence's tokens before the call and its rows per unit; rows 0: it sits out.
-__device__ __forceinline__ void sizes_of(const QuantView& L, const QuantAttention& io, int b, int& held, int& rows) {
-    held = rows = 0;
-    if (b >= L.batch) return;
-    const int len = io.len[b], count = io.count != nullptr ? min(io.count[b], io.queries) : io.queries;
-    if (len < 0 || count <= 0) return;
-    held = min(len, L.cap);
-    rows = count * L.G;
-}
-// Blocks that the call attends to (a step's new token counts if it finds a place).
-__device__ __forceinline__ int blocks_of(const QuantView& L, const QuantAttention& io, int held) {
-    return blocks_of(held + (io.k_new != nullptr && held < L.cap ? 1 : 0));
-}
-
-// Sum over this lane and those before it: within rows of 16 lanes by 1, 2, 4 and 8
-// places, then the last lane of a row, and of the lower half, onto those behind.
-__device__ __forceinline__ int scan_sum(int x) {
-    auto add = [&](auto ctrl, auto rows) {
-        x += __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
-    };
-    add(Int<0x111>(), Int<0xF>());
-    add(Int<0x112>(), Int<0xF>());
-    add(Int<0x114>(), Int<0xF>());
-    add(Int<0x118>(), Int<0xF>());
-    add(Int<0x142>(), Int<0xA>());
-    add(Int<0x143>(), Int<0xC>());
-    return x;
-}
-
-// The workgroup's work, or false where there is less than the grid allows for.
-template <int ROWS>
-__device__ __forceinline__ bool find_work(const QuantView& L, const QuantAttention& io, const Cut& cut, int lane, int wg,
-                                          Work& w) {
-    auto tiles_of = [](int rows) { return (rows + ROWS - 1) / ROWS; };
-    int t0 = 0, r0 = 0;
-    float cost = 0.0f;
-    for (int b = lane; b < L.batch; b += 64) {
-        sizes_of(L, io, b, t0, r0);
-        cost += (float)blocks_of(L, io, t0) * tiles_of(r0);
-    }
-    if (L.batch <= 64) sizes_of(L, io, lane, t0, r0);
-    cost = wave_sum(cost) * L.nkv;
-    const int chunk = max(cut.least, (int)ceilf(cost / cut.target));
-    auto parts_of = [&](int blocks) {
-        return max(1, min(kMaxQuantParts, (blocks + chunk - 1) / chunk));
-    };
-    int before = 0, slots = 0;
-    for (int b0 = 0; b0 < L.batch; b0 += 64) {
-        if (L.batch > 64) sizes_of(L, io, b0 + lane, t0, r0);
-        const int parts = parts_of(blocks_of(L, io, t0)), n = r0 > 0 ? L.nkv * tiles_of(r0) * parts : 0;
-        int upto = n, split = parts > 1 ? n : 0;
-        const int own = split;
-        upto = scan_sum(upto);
-        split = scan_sum(split);
-        const unsigned long long m = __ballot(wg < before + upto);
-        if (m == 0ull) {
-            before += __builtin_amdgcn_readlane(upto, 63);
-            slots += __builtin_amdgcn_readlane(split, 63);
-            continue;
-        }
-        const int at = __ffsll(m) - 1;
-        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-        w.b = b0 + at;
-        const int held = of(t0);
-        w.fresh = io.k_new != nullptr && held < L.cap ? held : -1;
-        w.tokens = held + (w.fresh >= 0 ? 1 : 0);
-        w.rows = of(r0);
-        w.parts = of(parts);
-        w.tiles = tiles_of(w.rows);
-        // KV heads innermost, so that with eight of them the tiles and parts of one
-        // meet on an XCD; the tiles that see the most tokens first
-        const int idx = wg - (before + of(upto) - of(n)), rest = idx / L.nkv;
-        w.h = idx - rest * L.nkv;
-        const int turn = rest / w.parts;
-        w.part = rest - turn * w.parts;
-        w.tile = w.tiles - 1 - turn;
-        // a tile's parts side by side
-        w.slot = slots + of(split) - of(own) + (w.h * w.tiles + w.tile) * w.parts;
-        return true;
-    }
-    return false;
-}
-
-// Workgroups that calls of up to these sizes may need.
-size_t most_workgroups(const Cut& cut, int row_tile, int batch, int queries, int nkv, int G) {
-    return (size_t)cut.target + (size_t)batch * nkv * ((queries * G + row_tile - 1) / row_tile);
-}
 
 // ---------------------------------------------------------------------------
 // The end of a tile: outputs and log-sum-exps of its rows 0 .. rows - 1 from
@@ -195,10 +30,7 @@ __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAtten
     const PrefixParts& pp = io.prefix;
     const size_t prows = (size_t)L.nkv * pp.rows, prow = (size_t)w.h * pp.rows + (size_t)w.b * L.G;
     const int parts = nsrc + pp.n;
-    auto to = [&](int row) {  // the row's place in out and lse
-        const int i = (row0 + row) / L.G, g = row0 + row - i * L.G;
-        return ((size_t)w.b * io.queries + i) * L.nkv * L.G + w.h * L.G + g;
-    };
+    auto to = [&](int row) { return row_at(L, io, w, row0 + row); };
     for (int row = wave_of(tid); row < rows; row += NW) {
         auto part_ml = [&](int s) {
             if (s < nsrc) return ml(s, row);
@@ -236,101 +68,6 @@ __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAtten
         ((T*)io.out)[to(row) * D + c] = from_f<T>(x);
     }
     __syncthreads();
-}
-
-// The softmax's reference need not be the maximum: it follows a row's logits once
-// they exceed it by this much (base 2), so that the sums stay within 2^kSlack of
-// their usual size and most blocks need no maximum over lanes. It starts at a
-// finite number far below every logit: the difference to a masked logit is then
-// -inf, never NaN.
-constexpr float kSlack = 8.0f, kLowest = -1e30f;
-
-// One block against RT tiles of 16 rows. A row of this lane's column sees tokens
-// below lim[t] of the block; `masked`: some row does not see all of them.
-template <typename T, int D, int KB, int VB, int RT>
-__device__ __forceinline__ void attend_block(const Block<D, KB, VB>& blk, const u32x4 (&q)[RT][D / 32][kQueryPieces<T>],
-                                             bool masked, const int (&lim)[RT], int a, float scale_log2,
-                                             Softmax<D> (&s)[RT]) {
-    constexpr int KS = D / 32, NQ = kQueryPieces<T>, NP = kProbPieces<T>;
-    f32x4 x[RT][2];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) x[t][0] = x[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const float scale = blk.key_scale(c);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const u32x4 k = blk.key(c, ks, scale);
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) x[t][c] = mfma(k, q[t][ks][n], x[t][c]);
-        }
-    }
-    if (masked) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[t][c][e] = 8 * a + 4 * c + e < lim[t] ? x[t][c][e] : -INFINITY;
-    }
-    float mb[RT];
-    bool over = false;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        mb[t] = x[t][0][0];
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mb[t] = fmaxf(mb[t], x[t][c][e]);
-        mb[t] *= scale_log2;
-        over = over || mb[t] > s[t].m + kSlack;
-    }
-    if (__ballot(over) != 0ull) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const float m = fmaxf(s[t].m, max_groups(mb[t]));
-            const float alpha = __builtin_amdgcn_exp2f(s[t].m - m);
-            s[t].l *= alpha;
-#pragma unroll
-            for (int ct = 0; ct < D / 16; ++ct) s[t].o[ct] *= alpha;
-            s[t].m = m;
-        }
-    }
-    Pieces<NP> p[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        float y[8], l = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][j >> 2][j & 3], scale_log2, -s[t].m));
-            l += y[j];
-        }
-        s[t].l += l;
-        p[t] = Pieces<NP>(y);
-    }
-    float vs[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) vs[j] = blk.value_scale(j);
-    auto two = [&](auto m) {
-        constexpr int M = decltype(m)::value;
-        u32x4 even, odd;
-        blk.template values<M>(vs, even, odd);
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int n = 0; n < NP; ++n) {
-                s[t].o[2 * M] = mfma(even, p[t].p[n], s[t].o[2 * M]);
-                s[t].o[2 * M + 1] = mfma(odd, p[t].p[n], s[t].o[2 * M + 1]);
-            }
-    };
-    two(Int<0>());
-    two(Int<1>());
-    if constexpr (D == 128) {
-        two(Int<2>());
-        two(Int<3>());
-    }
 }
 
 // A step's new token, quantised into the lanes that hold its place in the tail
@@ -412,10 +149,9 @@ __global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_
     Softmax<D> s[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int row = w.tile * TR + 16 * t + col, i = row / L.G, g = row - i * L.G;
+        const int row = w.tile * TR + 16 * t + col;
         const bool real = 16 * t + col < rows;
-        const size_t at = ((size_t)w.b * io.queries + i) * L.nkv * L.G + w.h * L.G + g;
-        load_query<T, D>((const T*)io.q + at * D, real, a, q[t]);
+        load_query<T, D>((const T*)io.q + row_at(L, io, w, row) * D, real, a, q[t]);
         lim[t] = real ? limit(row) : 0;
         s[t].clear();
         s[t].m = kLowest;
@@ -544,21 +280,26 @@ hipError_t launch(const QuantView& L, const QuantAttention& io, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Most rows per unit that the kernel for few takes.
+constexpr int kStreamRows = 32;
+
 }  // namespace
 
 QuantScratch quant_scratch(int batch, int queries, int nkv, int G) {
     // Every split tile has at least two parts of `chunk` blocks but for the last, and
     // all blocks together are at most target * chunk: at most 2 target slots.
-    auto tiles = [&](int r) { return (size_t)batch * nkv * ((queries * G + r - 1) / r); };
-    QuantScratch x{};
+    auto tiles = [&](int q, int r) { return (size_t)batch * nkv * ((q * G + r - 1) / r); };
+    QuantScratch x = quant_wide_scratch(batch, queries, nkv, G);
+    const int few = std::min(queries, kStreamRows / G);
     for (int r : {16, 32}) {
-        x.rows = std::max(x.rows, std::min((size_t)2 * kStreamCut.target, tiles(r) * kMaxQuantParts) * r);
-        x.arrivals = std::max(x.arrivals, tiles(r));
+        x.rows = std::max(x.rows, std::min((size_t)2 * kStreamCut.target, tiles(few, r) * kMaxQuantParts) * r);
+        x.arrivals = std::max(x.arrivals, tiles(few, r));
     }
     return x;
 }
 
 hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s) {
+    if (io.queries * L.G > kStreamRows) return launch_quant_wide(L, bf16, io, s);
     return with_types(L, bf16, [&](auto t, auto d, auto kb, auto vb) {
         return launch<decltype(t), d(), kb(), vb()>(L, io, s);
     });

@@ -35,6 +35,8 @@ namespace qnt {
 
 using namespace blk;
 
+template <int N>
+using Int = std::integral_constant<int, N>;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
@@ -62,47 +64,18 @@ struct Format {
 
 __device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
 
-// A lane's part of a block as it lies in memory.
+// A lane's keys of a block as they lie in memory.
 template <int D, int KB, int VB>
-struct Block {
+struct Keys {
     using F = Format<D, KB, VB>;
-    u32x4 k[F::NKP], v[F::NVP];
+    u32x4 k[F::NKP];
     uint32_t ke;  // exponents of the two tiles' keys
-    u32x2 ve;     // of the eight tokens' values
     __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
 #pragma unroll
         for (int p = 0; p < F::NKP; ++p) k[p] = ld16(rec + 1024 * p + 16 * lane);
-#pragma unroll
-        for (int p = 0; p < F::NVP; ++p) v[p] = ld16(rec + F::VALUES + 1024 * p + 16 * lane);
-        const int a = lane >> 4, i = lane & 15;
-        ke = *reinterpret_cast<const uint16_t*>(rec + F::KEXP + (F::kgroup(a) * 16 + i) * 2);
-        ve = *reinterpret_cast<const u32x2*>(rec + F::VEXP + (a * F::NG + F::vgroup(i)) * 8);
+        ke = *reinterpret_cast<const uint16_t*>(rec + F::KEXP + (F::kgroup(lane >> 4) * 16 + (lane & 15)) * 2);
     }
-    // Values of tokens `valid` .. of the block become 0, whatever is stored there.
-    __device__ __forceinline__ void zero_values_from(int valid, int a) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (8 * a + j >= valid) {
-                set_value(j, u32x2{0u, 0u});
-                set_exponent(j, 127u);
-            }
-    }
-    __device__ __forceinline__ void set_exponent(int j, uint32_t e) {
-        const int sh = 8 * (j & 3);
-        ve[j >> 2] = (ve[j >> 2] & ~(255u << sh)) | e << sh;
-    }
-    // Token j's codes of this lane's values (VBYTES of them).
-    __device__ __forceinline__ void set_value(int j, u32x2 c) {
-        if constexpr (F::VBYTES == 8) {
-            v[j >> 1][2 * (j & 1)] = c[0];
-            v[j >> 1][2 * (j & 1) + 1] = c[1];
-        } else if constexpr (F::VBYTES == 4) {
-            v[j >> 2][j & 3] = c[0];
-        } else {
-            const uint32_t x = v[0][j >> 1];
-            v[0][j >> 1] = j & 1 ? (x & 0xFFFFu) | c[0] << 16 : (x & 0xFFFF0000u) | (c[0] & 0xFFFFu);
-        }
-    }
+    __device__ __forceinline__ float key_scale(int q) const { return scale_of(q ? ke >> 8 : ke & 255u); }
     // Channels 8 ks .. 8 ks + 7 of this lane's key of tile q, as bf16.
     __device__ __forceinline__ u32x4 key(int q, int ks, float scale) const {
         u32x4 r;
@@ -123,22 +96,67 @@ struct Block {
         }
         return r;
     }
-    __device__ __forceinline__ float key_scale(int q) const { return scale_of(q ? ke >> 8 : ke & 255u); }
-    __device__ __forceinline__ float value_scale(int j) const { return scale_of(ve[j >> 2] >> (8 * (j & 3)) & 255u); }
-    // Channels 2 m and 2 m + 1 of this lane's values of token j, as bf16.
-    template <int M>
-    __device__ __forceinline__ uint32_t value2(int j, float scale) const {
-        if constexpr (VB == 4 && D == 128) {
-            return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[j >> 2][j & 3], scale, M));
-        } else if constexpr (VB == 4) {
+};
+
+// A lane's values of a block as they lie in memory.
+template <int D, int KB, int VB>
+struct Values {
+    using F = Format<D, KB, VB>;
+    u32x4 v[F::NVP];
+    u32x2 ve;  // exponents of the eight tokens
+    __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
+#pragma unroll
+        for (int p = 0; p < F::NVP; ++p) v[p] = ld16(rec + F::VALUES + 1024 * p + 16 * lane);
+        ve = *reinterpret_cast<const u32x2*>(rec + F::VEXP + ((lane >> 4) * F::NG + F::vgroup(lane & 15)) * 8);
+    }
+    // Tokens `valid` .. of the block become 0, whatever is stored there.
+    __device__ __forceinline__ void zero_values_from(int valid, int a) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (8 * a + j >= valid) {
+                set_value(j, u32x2{0u, 0u});
+                set_exponent(j, 120u);
+            }
+    }
+    __device__ __forceinline__ void set_exponent(int j, uint32_t e) {
+        const int sh = 8 * (j & 3);
+        ve[j >> 2] = (ve[j >> 2] & ~(255u << sh)) | e << sh;
+    }
+    // Token j's codes of this lane's values (VBYTES of them).
+    __device__ __forceinline__ void set_value(int j, u32x2 c) {
+        if constexpr (F::VBYTES == 8) {
+            v[j >> 1][2 * (j & 1)] = c[0];
+            v[j >> 1][2 * (j & 1) + 1] = c[1];
+        } else if constexpr (F::VBYTES == 4) {
+            v[j >> 2][j & 3] = c[0];
+        } else {
             const uint32_t x = v[0][j >> 1];
-            if (j & 1)
-                return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, M + 2));
-            return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, M));
+            v[0][j >> 1] = j & 1 ? (x & 0xFFFFu) | c[0] << 16 : (x & 0xFFFF0000u) | (c[0] & 0xFFFFu);
+        }
+    }
+    __device__ __forceinline__ uint32_t exponent(int j) const { return ve[j >> 2] >> (8 * (j & 3)) & 255u; }
+    __device__ __forceinline__ float value_scale(int j) const { return scale_of(exponent(j)); }
+    // Channels 2 M and 2 M + 1 of this lane's values of token j, as bf16 or (HALF) fp16.
+    template <int M, bool HALF = false>
+    __device__ __forceinline__ uint32_t value2(int j, float scale) const {
+        if constexpr (VB == 4) {
+            auto byte = [&](uint32_t x, auto n) {
+                if constexpr (HALF)
+                    return __builtin_bit_cast(uint32_t,
+                                              __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, decltype(n)::value));
+                else
+                    return __builtin_bit_cast(uint32_t,
+                                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, decltype(n)::value));
+            };
+            if constexpr (D == 128) return byte(v[j >> 2][j & 3], Int<M>());
+            else return j & 1 ? byte(v[0][j >> 1], Int<(M & 1) + 2>()) : byte(v[0][j >> 1], Int<M & 1>());
         } else {
             const int at = D == 128 ? 2 * j + M / 2 : j;
-            return __builtin_bit_cast(uint32_t,
-                                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[at >> 2][at & 3], scale, (M & 1) != 0));
+            const uint32_t x = v[at >> 2][at & 3];
+            if constexpr (HALF)
+                return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, scale, (M & 1) != 0));
+            else
+                return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, (M & 1) != 0));
         }
     }
     // All of this lane's values of token j.
@@ -154,14 +172,24 @@ struct Block {
     // Channels 2 M and 2 M + 1 of all eight tokens: two operands of the product
     // with probabilities (values come in pairs of channels of one token, operands
     // in pairs of tokens of one channel).
-    template <int M>
+    template <int M, bool HALF = false>
     __device__ __forceinline__ void values(const float (&scale)[8], u32x4& even, u32x4& odd) const {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint32_t x = value2<M>(2 * p, scale[2 * p]), y = value2<M>(2 * p + 1, scale[2 * p + 1]);
+            const uint32_t x = value2<M, HALF>(2 * p, scale[2 * p]), y = value2<M, HALF>(2 * p + 1, scale[2 * p + 1]);
             even[p] = __builtin_amdgcn_perm(y, x, 0x05040100u);
             odd[p] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
+    }
+};
+
+// A lane's part of a block.
+template <int D, int KB, int VB>
+struct Block : Keys<D, KB, VB>, Values<D, KB, VB> {
+    using F = Format<D, KB, VB>;
+    __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
+        Keys<D, KB, VB>::load(rec, lane);
+        Values<D, KB, VB>::load(rec, lane);
     }
 };
 
@@ -311,8 +339,6 @@ __device__ __forceinline__ uint8_t* record(const QuantView& L, int page, int blk
 }
 
 // Calls go with the types of the cache: go(element, head_dim, key bits, value bits).
-template <int N>
-using Int = std::integral_constant<int, N>;
 template <class Go>
 hipError_t with_types(const QuantView& L, bool bf16, Go go) {
     auto bits = [&](auto t, auto d) {

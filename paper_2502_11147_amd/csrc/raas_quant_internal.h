@@ -55,9 +55,9 @@ struct QuantAttention {
     void* v_held;
     PrefixParts prefix;    // n = 0: none (a step's only)
     float scale_log2;
-    // scratch: unnormalised outputs, maxima (base 2) and sums of units that are
-    // split, a slot of quant_tile_rows rows per workgroup; arrivals per unit and
-    // tile, zero between launches
+    // scratch: unnormalised outputs, maxima (base 2) and sums of tiles that are
+    // split, a slot of a tile's rows per workgroup; arrivals per unit and tile, zero
+    // between launches
     float* part;
     float* ml;
     int32_t* arrived;
@@ -71,6 +71,9 @@ struct QuantScratch {
     size_t arrivals;  // of arrived
 };
 QuantScratch quant_scratch(int batch, int queries, int nkv, int G);
+QuantScratch quant_wide_scratch(int batch, int queries, int nkv, int G);
 hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s);
+// Its kernels for many rows per unit.
+hipError_t launch_quant_wide(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s);
 
 }  // namespace raas

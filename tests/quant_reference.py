@@ -10,7 +10,10 @@ d (3 d) sums round: a logit is off by dx = (d + 4) u X, ((3 d + 4) u X), X = sum
 itself. An output is off by rel A, A = sum_j a_j |v_j|. In a bf16 cache the two
 bf16 pieces of a probability leave 2^-15 of it (less than 2^-7 after the first, of
 which the second is off by half a step, 2^-8), and the output is rounded, 2^-8 of
-its size. In an fp32 cache three pieces leave nothing, and their 3 n sums round."""
+its size. In calls of more than 32 rows per KV head a probability of a bf16 cache is
+one fp16 instead, off by half a step, 2^-11 of it, or, below 2^-14 of a unit that
+is at most 2^-7 of the largest (2^-21 of it), by 2^-25 of that unit: 2^-32 of the
+largest; the values beside it are exact. In an fp32 cache three pieces leave nothing, and their 3 n sums round."""
 from __future__ import annotations
 
 import math
@@ -53,8 +56,9 @@ def held(x, bits):
     return r.reshape(r.shape[:-2] + (-1,))
 
 
-def attention(q, K, V, bf16, prefix=None):
-    """(out, bound, lse, bound) of q [rows][d] over held K, V [n][d] (n may be 0) and a prefix's."""
+def attention(q, K, V, bf16, prefix=None, half=False):
+    """(out, bound, lse, bound) of q [rows][d] over held K, V [n][d] (n may be 0) and a
+    prefix's; half: probabilities are fp16."""
     if prefix is not None:
         K, V = np.concatenate([K, prefix[0]]), np.concatenate([V, prefix[1]])
     rows, d = q.shape
@@ -71,7 +75,8 @@ def attention(q, K, V, bf16, prefix=None):
     out, A = a @ V, a @ np.abs(V)
     bound = rel[:, None] * A + 2 * U32 * np.abs(out) + 1e-37
     if bf16:
-        bound = bound + 2.0 ** -15 * A
+        bound = bound + (2.0 ** -11 * A + 2.0 ** -32 * a.max(axis=1, keepdims=True) * np.abs(V).sum(axis=0) if half
+                         else 2.0 ** -15 * A)
         bound = bound + 2.0 ** -8 * (np.abs(out) + bound)
     lse = (m + np.log(z))[:, 0]
     return out, bound, lse, rel + 8 * U32 * (np.abs(lse) + np.log(z)[:, 0] + 1.0)

@@ -238,7 +238,7 @@ class Model:
                     if seen is not None:
                         K, V = K[seen(b, last)], V[seen(b, last)]
                     heads = slice(h * G, (h + 1) * G)
-                    o, ob, l, lb = ref.attention(qn[b, i, heads], K, V, self.bf16)
+                    o, ob, l, lb = ref.attention(qn[b, i, heads], K, V, self.bf16, half=n * G > 32)
                     _within(got[b, i, heads], o, ob, ("out", b, i, h))
                     _within(gl[b, i, heads], l, lb, ("lse", b, i, h))
         return out, lse
@@ -414,6 +414,51 @@ def test_ragged_batches(lens):
     m.attend(1)
     m.step(active=[b % 5 != 1 for b in range(len(lens))])
     m.attend(3, counts=[b % 4 for b in range(len(lens))])
+
+
+@gpu
+@pytest.mark.parametrize("hq,queries,d,dtype", [(4, 40, 64, "bf16"), (6, 97, 128, "bf16"), (2, 60, 64, "f32"), (4, 45, 128, "f32")], ids=str)
+@pytest.mark.parametrize("bits", BITS, ids=str)
+def test_pieces_of_long_prompts(bits, hq, queries, d, dtype):
+    """Many rows over many blocks: tiles cut into parts, tables without some pages, stale NaN
+    behind the last token, sequences of no or few tokens and queries beside them."""
+    import torch
+
+    lens = [2500, 700, 0, 33, 90]
+    m = Model([0] * 5, hq, 2 if hq != 6 else 1, d, bits, dtype, page=32, width=80, max_queries=queries, spare=2)
+    nan = torch.full((5, m.hkv, 80 * 32, d), float("nan"), dtype=m.dt, device="cuda")
+    m.cache.write(0, nan, nan, m.table, _ints([0] * 5))
+    m.write(lens)
+    m.attend(queries, counts=[queries, queries - 1, queries, queries, 3])
+    m.pages[0, 3], m.pages[0, 77], m.pages[1, 21], m.pages[3, 0] = -1, m.cache.n_pages, -7, -1
+    m.table = _ints(m.pages)
+    good = [np.repeat((p >= 0) & (p < m.cache.n_pages), 32) for p in m.pages]
+    m.attend(queries, counts=[queries, 1, 0, 20, queries], seen=lambda b, last: good[b][:last])
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("queries", [1, 40])
+def test_values_of_any_scale(queries, bits, d):
+    """Values far from 1, in whole sequences, single blocks, tokens and groups: probabilities
+    and values in fp16 give way to bf16 there."""
+    m = Model([0] * 5, 4, 2, d, bits, page=32, width=12, max_queries=queries)
+    n = 300
+    k, kn = m.data(5, 2, n, d)
+    v = m.rng.standard_normal((5, 2, n, d)).astype(np.float32)
+    v[0] *= 2.0 ** 60
+    v[1] *= 2.0 ** -60
+    v[2, :, 64:96] *= 2.0 ** 40
+    v[3, 0, 200] *= 2.0 ** -45
+    v[3, 1, 17, :32] *= 2.0 ** 50
+    v[4, :, 290:] = 0
+    v = _dev(v, m.dt)
+    m.cache.write(0, k, v, m.table, _ints([0] * 5))
+    for b in range(5):
+        m.K[b], m.V[b] = ref.held(kn[b], bits[0]), ref.held(_np(v)[b], bits[1])
+    m.attend(queries)
+    m.attend(queries, lens=[299, 65, 70, 300, 290])
 
 
 @gpu
