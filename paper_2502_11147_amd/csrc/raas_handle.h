@@ -70,6 +70,15 @@ inline raas_status check_creation(void* stream) {
     return RAAS_OK;
 }
 
+// Whether a step reads its layer of `own` bytes with non-temporal loads, which
+// leave the memory-side cache (256 MB) alone: where too little of the layer is
+// still there (us per step, ordinary / non-temporal: 268 MB alone 47.1 / 48.7,
+// in turn with two more caches of that size 58.3 / 52.9; 134 MB 38.0 / 41.8 and
+// 45.8 / 43.4; 67 MB 21.7 / 22.9 and 21.8 / 23.8; 403 MB alone 84.4 / 70.5; with a
+// prefix in front, its attention included: 268 MB and a prefix of 134 MB 100.0 /
+// 90.5, 67 MB and 268 MB 85.0 / 79.6).
+inline bool non_temporal(double own, double others) { return others + own * 2.0 / 3.0 > 256e6; }
+
 // A part of a handle's memory; `clear`: it starts at zero.
 struct Req {
     void** ptr;

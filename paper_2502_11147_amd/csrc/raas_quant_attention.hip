@@ -21,7 +21,7 @@ using namespace qnt;
 // The end of a tile: outputs and log-sum-exps of its rows 0 .. rows - 1 from
 // `nsrc` disjoint parts of the tokens (ml: reference and sum, o: unnormalised
 // outputs) and those of the prefix. A wavefront per row, a lane per part finds the
-// shares; then a thread per output element. s_w: [nsrc + prefix parts][16].
+// shares; then a thread per four channels. s_w: [nsrc + prefix parts][16].
 constexpr int kFinishSources = kMaxQuantParts + kMaxPrefixParts;
 template <typename T, int D, int NW, class Ml, class O>
 __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAttention& io, const Work& w, int row0,
@@ -48,24 +48,28 @@ __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAtten
             io.lse[to(row)] = Z > 0.0f ? (M + __builtin_amdgcn_logf(Z)) * 0.69314718055994530942f : -INFINITY;
     }
     __syncthreads();
-    for (int e = tid; e < rows * D; e += NW * 64) {
-        const int row = e / D, c = e % D;
-        float x = 0.0f;
-        for (int s0 = 0; s0 < nsrc; s0 += 8) {  // eight on their way together
-            float y[8];
+    typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    constexpr int AHEAD = 16;  // reads on their way together
+    for (int e = tid; e < rows * (D / 4); e += NW * 64) {
+        const int row = e / (D / 4), c = e % (D / 4) * 4;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        auto add = [&](int n, int w0, auto value) {
+            for (int s0 = 0; s0 < n; s0 += AHEAD) {
+                f32x4 y[AHEAD];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = o(min(s0 + k, nsrc - 1), row, c);
+                for (int k = 0; k < AHEAD; ++k)
+                    y[k] = value(min(s0 + k, n - 1));
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x = __builtin_fmaf(y[k], s0 + k < nsrc ? s_w[s0 + k][row] : 0.0f, x);
-        }
-        for (int s0 = 0; s0 < pp.n; s0 += 8) {
-            float y[8];
+                for (int k = 0; k < AHEAD; ++k)
+                    x += y[k] * (s0 + k < n ? s_w[w0 + s0 + k][row] : 0.0f);
+            }
+        };
+        add(nsrc, 0, [&](int k) { return o(k, row, c); });
+        add(pp.n, nsrc, [&](int k) { return *reinterpret_cast<const f32x4*>(pp.o + (k * prows + prow + row) * D + c); });
+        T4 y;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = pp.o[(min(s0 + k, pp.n - 1) * prows + prow + row) * D + c];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x = __builtin_fmaf(y[k], s0 + k < pp.n ? s_w[nsrc + s0 + k][row] : 0.0f, x);
-        }
-        ((T*)io.out)[to(row) * D + c] = from_f<T>(x);
+        for (int k = 0; k < 4; ++k) y[k] = from_f<T>(x[k]);
+        *reinterpret_cast<T4*>((T*)io.out + to(row) * D + c) = y;
     }
     __syncthreads();
 }
@@ -128,14 +132,23 @@ __device__ __forceinline__ void take_token(const QuantAttention& io, Block<D, KB
 // and write the outputs, or publish the part: the last of a tile's parts to end
 // joins them all. Pages of a wavefront's next 64 blocks lie in its lanes.
 constexpr int kStreamWaves = 4;
-template <typename T, int RT>
-constexpr int kStreamPerSimd = sizeof(T) == 4 ? 1 : RT == 1 ? 3 : 2;
-constexpr Cut kStreamCut = {768, 2 * kStreamWaves};
+// Blocks of a wavefront on their way or in use, and wavefronts per SIMD. A layer
+// that streams from memory in 4 bits (128 sequences of 8192 tokens) takes 221 us
+// with two and three, 198 with non-temporal loads, 181 with four and two besides;
+// caches that stay near are no faster so (49 and 52 us, 64 sequences of 4096), nor
+// are 8 bits (91 and 92), whose blocks are twice as large.
+template <typename T, int KB, int VB, bool STREAM>
+constexpr int kStreamBlocks = STREAM && KB + VB == 8 && sizeof(T) == 2 ? 4 : 2;
+template <typename T, int KB, int VB, bool STREAM>
+constexpr int kStreamPerSimd = sizeof(T) == 4 ? 1 : kStreamBlocks<T, KB, VB, STREAM> == 4 ? 2 : 3;
+constexpr Cut kStreamCut = {256, 8};
 
-template <typename T, int D, int KB, int VB, int RT>
-__global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, RT>))) void k_quant_stream(QuantView L, QuantAttention io) {
+template <typename T, int D, int KB, int VB, bool STREAM>
+__global__ __launch_bounds__(kStreamWaves * 64)
+__attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_quant_stream(QuantView L,
+                                                                                            QuantAttention io) {
     using F = Format<D, KB, VB>;
-    constexpr int NW = kStreamWaves, TR = 16 * RT;
+    constexpr int NW = kStreamWaves, RT = 1, TR = 16, NB = kStreamBlocks<T, KB, VB, STREAM>;
     __shared__ __align__(16) float s_o[NW][16][D + 4];
     __shared__ float s_m[NW][16], s_l[NW][16], s_w[kFinishSources][16];
     const int tid = threadIdx.x, lane = tid & 63, wv = wave_of(tid), a = lane >> 4, col = lane & 15;
@@ -168,14 +181,15 @@ __global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_
     // This wavefront's blocks. The sequence's last one, if it is here, comes last, and
     // only it takes a new token or ends with places that hold none.
     const int turns = lo + wv < hi ? (hi - lo - wv + NW - 1) / NW : 0;
-    Block<D, KB, VB> b0, b1;
-    // page of the turn's block, -1: none; the block (of no page: any, unused)
-    auto fetch = [&](int turn, Block<D, KB, VB>& blk) {
+    Block<D, KB, VB> ring[NB];
+    int page[NB];
+    // the block, and its page, -1: none (then the block is any, unused)
+    auto fetch = [&](int turn, auto i) {
+        constexpr int I = decltype(i)::value;
         if ((turn & 63) == 0) window(turn);
-        int page = __builtin_amdgcn_readlane(win, turn & 63);
-        page = page >= 0 && page < L.n_pages ? page : -1;
-        blk.load(record<F>(L, max(page, 0), lo + wv + turn * NW, w.h), lane);
-        return page;
+        page[I] = __builtin_amdgcn_readlane(win, turn & 63);
+        page[I] = page[I] >= 0 && page[I] < L.n_pages ? page[I] : -1;
+        ring[I].template load<STREAM>(record<F>(L, max(page[I], 0), lo + wv + turn * NW, w.h), lane);
     };
     auto attend = [&](int b, Block<D, KB, VB>& blk) {
         const int t0 = b * kQuantBlock;
@@ -185,25 +199,40 @@ __global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_
         attend_block<T, D, KB, VB, RT>(blk, q, t0 + kQuantBlock > least, l, a, io.scale_log2, s);
     };
     if (turns > 0) {
-        int p0 = fetch(0, b0), turn = 0;
-        while (turn + 1 < turns) {
-            const int p1 = fetch(turn + 1, b1);
-            if (p0 >= 0) attend(lo + wv + turn * NW, b0);
-            if (++turn + 1 >= turns) {
-                b0 = b1;
-                p0 = p1;
-                break;
+        fetch(0, Int<0>());
+        if constexpr (NB > 2) fetch(1, Int<1>());
+        if constexpr (NB > 3) fetch(2, Int<2>());
+        // one turn at place I of the ring; false: it is the last one's, which is left there
+        int turn = 0;
+        auto pass = [&](auto i) {
+            constexpr int I = decltype(i)::value, LAST = (I + NB - 1) % NB;
+            if (turn + 1 >= turns) {
+                if constexpr (I > 0) {
+                    ring[0] = ring[I];
+                    page[0] = page[I];
+                }
+                return false;
             }
-            p0 = fetch(turn + 1, b0);
-            if (p1 >= 0) attend(lo + wv + turn * NW, b1);
+            fetch(turn + NB - 1, Int<LAST>());
+            if (page[I] >= 0) attend(lo + wv + turn * NW, ring[I]);
             ++turn;
+            return true;
+        };
+        for (;;) {
+            if (!pass(Int<0>()) || !pass(Int<1>())) break;
+            if constexpr (NB > 2)
+                if (!pass(Int<2>())) break;
+            if constexpr (NB > 3)
+                if (!pass(Int<3>())) break;
         }
-        if (p0 >= 0) {
+        if (page[0] >= 0) {
+            Block<D, KB, VB>& blk = ring[0];
             const int b = lo + wv + turn * NW, t0 = b * kQuantBlock;
             if (w.fresh >= t0 && w.fresh < t0 + kQuantBlock)
-                take_token<T, D, KB, VB>(io, b0, record<F>(L, p0, b, w.h), w.fresh - t0, (size_t)w.b * L.nkv + w.h, lane);
-            if (t0 + kQuantBlock > w.tokens) b0.zero_values_from(w.tokens - t0, a);
-            attend(b, b0);
+                take_token<T, D, KB, VB>(io, blk, record<F>(L, page[0], b, w.h), w.fresh - t0, (size_t)w.b * L.nkv + w.h,
+                                         lane);
+            if (t0 + kQuantBlock > w.tokens) blk.zero_values_from(w.tokens - t0, a);
+            attend(b, blk);
         }
     }
     const bool split = w.parts > 1;
@@ -228,22 +257,23 @@ __global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_
         auto ml = [&](int k, int row) { return make_float2(s_m[k][row], s_l[k][row]); };
         if (!split) {
             finish_rows<T, D, NW>(L, io, w, first + 16 * t, here, tid, NW, s_w, ml,
-                                  [&](int k, int row, int c) { return s_o[k][row][c]; });
+                                  [&](int k, int row, int c) { return *reinterpret_cast<const f32x4*>(&s_o[k][row][c]); });
             continue;
         }
         const size_t slot = (size_t)(w.slot + w.part) * TR + 16 * t;
-        for (int e = tid; e < here * D; e += NW * 64) {
-            const int row = e / D, c = e % D;
-            float M = kLowest, x = 0.0f, z = 0.0f;
+        for (int e = tid; e < here * (D / 4); e += NW * 64) {
+            const int row = e / (D / 4), c = e % (D / 4) * 4;
+            float M = kLowest, z = 0.0f;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < NW; ++k) M = fmaxf(M, s_m[k][row]);
 #pragma unroll
             for (int k = 0; k < NW; ++k) {
                 const float share = __builtin_amdgcn_exp2f(s_m[k][row] - M);
-                x = __builtin_fmaf(s_o[k][row][c], share, x);
+                x += *reinterpret_cast<const f32x4*>(&s_o[k][row][c]) * share;
                 z = __builtin_fmaf(s_l[k][row], share, z);
             }
-            publish(io.part + (slot + row) * D + c, x);
+            publish4(io.part + (slot + row) * D + c, x);
             if (c == 0) {
                 publish(io.ml + 2 * (slot + row), M);
                 publish(io.ml + 2 * (slot + row) + 1, z);
@@ -264,24 +294,23 @@ __global__ __launch_bounds__(kStreamWaves * 64) __attribute__((amdgpu_waves_per_
             [&](int k, int row) {
                 return make_float2(published(io.ml + 2 * at(k, row)), published(io.ml + 2 * at(k, row) + 1));
             },
-            [&](int k, int row, int c) { return published(io.part + at(k, row) * D + c); });
+            [&](int k, int row, int c) { return published4(io.part + at(k, row) * D + c); });
     }
 }
 
 template <typename T, int D, int KB, int VB>
-hipError_t launch(const QuantView& L, const QuantAttention& io, hipStream_t s) {
-    const int rows = io.queries * L.G;
-    auto go = [&](auto kernel, int tile) {
-        const size_t grid = most_workgroups(kStreamCut, tile, L.batch, io.queries, L.nkv, L.G);
+hipError_t launch(const QuantView& L, const QuantAttention& io, bool stream, hipStream_t s) {
+    const size_t grid = most_workgroups(kStreamCut, 16, L.batch, io.queries, L.nkv, L.G);
+    auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kStreamWaves * 64), 0, s, L, io);
     };
-    if (rows <= 16) go(k_quant_stream<T, D, KB, VB, 1>, 16);
-    else go(k_quant_stream<T, D, KB, VB, 2>, 32);
+    if (stream) go(k_quant_stream<T, D, KB, VB, true>);
+    else go(k_quant_stream<T, D, KB, VB, false>);
     return hipGetLastError();
 }
 
 // Most rows per unit that the kernel for few takes.
-constexpr int kStreamRows = 32;
+constexpr int kStreamRows = 16;
 
 }  // namespace
 
@@ -291,17 +320,16 @@ QuantScratch quant_scratch(int batch, int queries, int nkv, int G) {
     auto tiles = [&](int q, int r) { return (size_t)batch * nkv * ((q * G + r - 1) / r); };
     QuantScratch x = quant_wide_scratch(batch, queries, nkv, G);
     const int few = std::min(queries, kStreamRows / G);
-    for (int r : {16, 32}) {
-        x.rows = std::max(x.rows, std::min((size_t)2 * kStreamCut.target, tiles(few, r) * kMaxQuantParts) * r);
-        x.arrivals = std::max(x.arrivals, tiles(few, r));
-    }
+    const size_t t = tiles(few, 16);
+    x.rows = std::max(x.rows, std::min((size_t)2 * kStreamCut.target, t * kMaxQuantParts) * 16);
+    x.arrivals = t;
     return x;
 }
 
-hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s) {
+hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, bool stream, hipStream_t s) {
     if (io.queries * L.G > kStreamRows) return launch_quant_wide(L, bf16, io, s);
     return with_types(L, bf16, [&](auto t, auto d, auto kb, auto vb) {
-        return launch<decltype(t), d(), kb(), vb()>(L, io, s);
+        return launch<decltype(t), d(), kb(), vb()>(L, io, stream, s);
     });
 }
 

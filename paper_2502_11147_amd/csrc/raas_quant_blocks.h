@@ -64,15 +64,21 @@ struct Format {
 
 __device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
 
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const uint8_t* p) {
+    return NT ? ld16_nt(p) : ld16(p);
+}
+
 // A lane's keys of a block as they lie in memory.
 template <int D, int KB, int VB>
 struct Keys {
     using F = Format<D, KB, VB>;
     u32x4 k[F::NKP];
     uint32_t ke;  // exponents of the two tiles' keys
+    template <bool NT>
     __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
 #pragma unroll
-        for (int p = 0; p < F::NKP; ++p) k[p] = ld16(rec + 1024 * p + 16 * lane);
+        for (int p = 0; p < F::NKP; ++p) k[p] = load16<NT>(rec + 1024 * p + 16 * lane);
         ke = *reinterpret_cast<const uint16_t*>(rec + F::KEXP + (F::kgroup(lane >> 4) * 16 + (lane & 15)) * 2);
     }
     __device__ __forceinline__ float key_scale(int q) const { return scale_of(q ? ke >> 8 : ke & 255u); }
@@ -104,9 +110,10 @@ struct Values {
     using F = Format<D, KB, VB>;
     u32x4 v[F::NVP];
     u32x2 ve;  // exponents of the eight tokens
+    template <bool NT>
     __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
 #pragma unroll
-        for (int p = 0; p < F::NVP; ++p) v[p] = ld16(rec + F::VALUES + 1024 * p + 16 * lane);
+        for (int p = 0; p < F::NVP; ++p) v[p] = load16<NT>(rec + F::VALUES + 1024 * p + 16 * lane);
         ve = *reinterpret_cast<const u32x2*>(rec + F::VEXP + ((lane >> 4) * F::NG + F::vgroup(lane & 15)) * 8);
     }
     // Tokens `valid` .. of the block become 0, whatever is stored there.
@@ -183,13 +190,14 @@ struct Values {
     }
 };
 
-// A lane's part of a block.
+// A lane's part of a block. NT: codes are read with non-temporal loads.
 template <int D, int KB, int VB>
 struct Block : Keys<D, KB, VB>, Values<D, KB, VB> {
     using F = Format<D, KB, VB>;
+    template <bool NT = false>
     __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
-        Keys<D, KB, VB>::load(rec, lane);
-        Values<D, KB, VB>::load(rec, lane);
+        Keys<D, KB, VB>::template load<NT>(rec, lane);
+        Values<D, KB, VB>::template load<NT>(rec, lane);
     }
 };
 

@@ -72,7 +72,8 @@ struct QuantScratch {
 };
 QuantScratch quant_scratch(int batch, int queries, int nkv, int G);
 QuantScratch quant_wide_scratch(int batch, int queries, int nkv, int G);
-hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s);
+// stream: codes are read with non-temporal loads
+hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, bool stream, hipStream_t s);
 // Its kernels for many rows per unit.
 hipError_t launch_quant_wide(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s);
 

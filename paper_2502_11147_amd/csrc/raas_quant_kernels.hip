@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_quant_read(QuantView L, QuantCo
     Span s;
     if (!s.find(L, io, b, blockIdx.x * kWaves + wave_of(threadIdx.x))) return;
     Block<D, KB, VB> o;
-    o.load(record<F>(L, s.page, s.blk, h), lane);
+    o.template load<true>(record<F>(L, s.page, s.blk, h), lane);
     const size_t row0 = ((size_t)b * L.nkv + h) * io.stride;
     auto in = [&](int t) { return t >= s.lo && t < s.hi; };
     auto row = [&](void* x, int t) { return (T*)x + (row0 + (t + s.shift)) * D; };

@@ -27,6 +27,7 @@ struct raas_quant_cache {
     float *part = nullptr, *ml = nullptr;
     int32_t* arrived = nullptr;
     size_t bytes = 0;
+    std::vector<unsigned long long> streamed_at;  // count_streamed after each layer's last attention; 0: none yet
     hipStream_t last_stream = nullptr;
 };
 
@@ -79,19 +80,27 @@ raas_status copy(raas_quant_cache* c, int32_t layer, const void* k, const void* 
     return RAAS_OK;
 }
 
-// The attention of a call, and what it reads counted among the steps' reads: at
-// most the pages of the table, and the pool (lengths are not known here).
-raas_status attention(raas_quant_cache* c, const QuantView& L, QuantAttention& io, hipStream_t s) {
+// The attention of a call. What it reads is counted among the steps' reads: the
+// table's pages, or the pool if that is less (lengths are not known here). By what
+// was read since the layer's last attention its codes are still in the memory-side
+// cache or not; a captured call, whose replays are not seen here, counts the cache's
+// other layers, and `prefix_bytes` for each.
+raas_status attention(raas_quant_cache* c, int32_t layer, const QuantView& L, QuantAttention& io, double prefix_bytes,
+                      hipStream_t s) {
     io.scale_log2 = scale_log2(L.D);
     io.part = c->part;
     io.ml = c->ml;
     io.arrived = c->arrived;
-    const hipError_t e = launch_quant_attention(L, c->bf16, io, s);
-    if (e != hipSuccess) return hip_fail(e, "attention launch");
+    const double page = (double)(c->layer_bytes / L.n_pages);
+    const double own = page * std::min((double)L.n_pages, (double)L.batch * L.width);
+    double others = (c->cfg.n_layers - 1.0) * own + c->cfg.n_layers * prefix_bytes;
     if (!capturing(s)) {
-        const unsigned long long page = c->layer_bytes / L.n_pages;
-        count_streamed(c->device, page * std::min<unsigned long long>(L.n_pages, (unsigned long long)L.batch * L.width));
+        const unsigned long long before = count_streamed(c->device, (unsigned long long)own);
+        if (c->streamed_at[layer] != 0) others = (double)(before - c->streamed_at[layer]);
+        c->streamed_at[layer] = before + (unsigned long long)own;
     }
+    const hipError_t e = launch_quant_attention(L, c->bf16, io, non_temporal(own, others), s);
+    if (e != hipSuccess) return hip_fail(e, "attention launch");
     c->last_stream = s;
     return RAAS_OK;
 }
@@ -127,6 +136,7 @@ raas_status raas_create_quant_cache(const raas_quant_config* cfg, void* stream, 
     try {
         c = new raas_quant_cache();
         c->cfg = *cfg;
+        c->streamed_at.assign((size_t)cfg->n_layers, 0);
         c->bf16 = cfg->dtype == RAAS_BF16;
         const hipError_t e = hipGetDevice(&c->device);
         if (e != hipSuccess) {
@@ -200,7 +210,7 @@ raas_status raas_quant_attention(raas_quant_cache* c, int32_t layer, const void*
     io.len = lens;
     io.count = counts;
     io.queries = queries;
-    return attention(c, L, io, (hipStream_t)stream);
+    return attention(c, layer, L, io, 0.0, (hipStream_t)stream);
 }
 
 raas_status raas_quant_step(raas_quant_cache* c, int32_t layer, const void* q, const void* k_new, const void* v_new,
@@ -229,11 +239,12 @@ raas_status raas_quant_step(raas_quant_cache* c, int32_t layer, const void* q, c
     io.v_new = v_new;
     io.k_held = k_held;
     io.v_held = v_held;
+    double prefix_bytes = 0.0;
     if (prefix) {
-        st = step_prefix_parts(prefix, layer, q, batch, io.prefix, (hipStream_t)stream);
+        st = step_prefix_parts(prefix, layer, q, batch, io.prefix, prefix_bytes, (hipStream_t)stream);
         if (st != RAAS_OK) return st;
     }
-    return attention(c, L, io, (hipStream_t)stream);
+    return attention(c, layer, L, io, prefix_bytes, (hipStream_t)stream);
 }
 
 }  // extern "C"

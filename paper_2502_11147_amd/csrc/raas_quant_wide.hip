@@ -5,7 +5,6 @@
 
 #include "raas_quant_attention.h"
 
-
 namespace raas {
 namespace {
 
@@ -13,14 +12,15 @@ using namespace qnt;
 
 // A wavefront is a workgroup: it takes a tile of 16 RT rows through the blocks of
 // its part, straight from memory to registers, converts them there and shares
-// nothing. (Through LDS, where eight wavefronts of 32 rows convert each block once
-// for all, reading it back took as long as the products, and the barrier of every
-// block as long again: a tile's 32 rows took 2616 cycles a block on a SIMD.)
+// nothing. (Through LDS, where eight wavefronts converted each block once for all of
+// them, 512 rows of four long prompts took 579 us against 632, but a prompt of 4096
+// tokens 179 against 168, 256 tokens behind 1000 41 against 35: reading it back, and
+// a barrier for every two blocks, took most of what it saved.)
 template <typename T>
 constexpr int kRowTiles = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
 constexpr int kWideRows = 16 * kRowTiles<T>;
-constexpr Cut kWideCut = {2048, 8};
+constexpr Cut kWideCut = {1024, 8};
 
 // Beside a bf16 cache's values, probabilities are rounded to fp16 (half a step,
 // 2^-11 of themselves, an eighth of what the rounding of a bf16 output may be; in
@@ -28,18 +28,18 @@ constexpr Cut kWideCut = {2048, 8};
 // then fp16 too: codes times X / 2^(kUnit - 127), exact while X's exponent byte lies
 // in kLeast .. kLeast + kSpan - 1: the least step of a code is 2^-20 (2^-21) there,
 // the largest value 7168 (12288). A wavefront that meets another exponent starts over
-// with attend_block, two products. Probabilities are taken relative to 2^-kRaise of the row's maximum at the time, so
-// they lie below 2^(kRaise + kSlack) and keep all digits down to 2^-14:
-// 2^-21 of the largest or less; below, they are off by 2^-25.
+// with attend_block, two products. Probabilities are taken relative to 2^-kRaise of
+// the row's maximum at the time, so they lie below 2^(kRaise + kSlack) and keep all
+// digits down to 2^-14: 2^-21 of the largest or less; below, they are off by 2^-25.
 template <int VB>
 struct Half {
     static constexpr int kUnit = VB == 4 ? 128 : 120, kLeast = VB == 4 ? 108 : 109, kSpan = VB == 4 ? 32 : 16;
     // Whether one of these exponents lies outside (a byte below kLeast borrows from the
     // next one, but is outside itself).
-    static __device__ __forceinline__ bool outside(u32x2 e) {
-        constexpr uint32_t each = 0x01010101u;
-        return (((e[0] - each * kLeast) | (e[1] - each * kLeast)) & (each * (256u - kSpan))) != 0u;
+    static __device__ __forceinline__ uint32_t beyond(uint32_t e) {
+        return (e - 0x01010101u * kLeast) & (0x01010101u * (256u - kSpan));
     }
+    static __device__ __forceinline__ bool outside(u32x2 e) { return (beyond(e[0]) | beyond(e[1])) != 0u; }
 };
 constexpr float kRaise = 7.0f;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -267,10 +267,12 @@ __global__ __launch_bounds__(256) void k_quant_join(QuantView L, QuantAttention 
 template <typename T, int D, int KB, int VB>
 hipError_t launch(const QuantView& L, const QuantAttention& io, hipStream_t s) {
     const size_t grid = most_workgroups(kWideCut, kWideRows<T>, L.batch, io.queries, L.nkv, L.G);
-    const size_t rows = (size_t)L.batch * L.nkv * io.queries * L.G;
     hipLaunchKernelGGL((k_quant_wide<T, D, KB, VB>), dim3((unsigned)grid), dim3(64), 0, s, L, io);
-    hipLaunchKernelGGL((k_quant_join<T, D>), dim3((unsigned)std::min((rows + 3) / 4, (size_t)kJoinWorkgroups)), dim3(256), 0,
-                       s, L, io);
+    if (L.cap / kQuantBlock > kWideCut.least) {  // (else no part is cut)
+        const size_t rows = (size_t)L.batch * L.nkv * io.queries * L.G;
+        hipLaunchKernelGGL((k_quant_join<T, D>), dim3((unsigned)std::min((rows + 3) / 4, (size_t)kJoinWorkgroups)),
+                           dim3(256), 0, s, L, io);
+    }
     return hipGetLastError();
 }
 

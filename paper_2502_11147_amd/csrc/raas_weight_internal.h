@@ -103,12 +103,13 @@ hipError_t launch_prefix_attention(const PrefixView& P, bool bf16, const void* q
 hipError_t launch_prefix_join(const PrefixView& P, bool bf16, void* out, float* lse, hipStream_t s);
 
 // A cache whose step attends to a shared prefix besides, and the refusals that
-// follow; then the prefix's attention of the step's queries into its parts.
+// follow; then the prefix's attention of the step's queries into its parts, and the bytes
+// that it reads.
 struct PrefixUser {
     int n_q_heads, n_kv_heads, head_dim, dtype, device, batch;
 };
 raas_status check_step_prefix(const raas_prefix* p, int32_t layer, const PrefixUser& u);
-raas_status step_prefix_parts(raas_prefix* p, int32_t layer, const void* q, int batch, PrefixParts& parts,
+raas_status step_prefix_parts(raas_prefix* p, int32_t layer, const void* q, int batch, PrefixParts& parts, double& bytes,
                               hipStream_t s);
 
 // Keys and values of units to blocks: row t of unit u comes from row

@@ -99,15 +99,6 @@ raas_status check_layer(const raas_prefix* p, int32_t layer) {
     return RAAS_OK;
 }
 
-// Whether a step reads its layer of `own` bytes with non-temporal loads, which
-// leave the memory-side cache (256 MB) alone: where too little of the layer is
-// still there (us per step, ordinary / non-temporal: 268 MB alone 47.1 / 48.7,
-// in turn with two more caches of that size 58.3 / 52.9; 134 MB 38.0 / 41.8 and
-// 45.8 / 43.4; 67 MB 21.7 / 22.9 and 21.8 / 23.8; 403 MB alone 84.4 / 70.5; with a
-// prefix in front, its attention included: 268 MB and a prefix of 134 MB 100.0 /
-// 90.5, 67 MB and 268 MB 85.0 / 79.6).
-bool non_temporal(double own, double others) { return others + own * 2.0 / 3.0 > 256e6; }
-
 // Bytes of keys and values that attention over a layer of the prefix reads.
 double prefix_bytes(const raas_prefix* p, int32_t layer) {
     return 2.0 * p->cfg.n_kv_heads * pad_tokens(p->stored[layer], p->bf16) * p->cfg.head_dim * (p->bf16 ? 2 : 4);
@@ -183,9 +174,10 @@ raas_status check_step_prefix(const raas_prefix* p, int32_t layer, const PrefixU
     return RAAS_OK;
 }
 
-raas_status step_prefix_parts(raas_prefix* p, int32_t layer, const void* q, int batch, PrefixParts& parts,
+raas_status step_prefix_parts(raas_prefix* p, int32_t layer, const void* q, int batch, PrefixParts& parts, double& bytes,
                               hipStream_t s) {
     PrefixView P;
+    bytes = prefix_bytes(p, layer);
     const raas_status st = prefix_parts(p, layer, q, batch, P, s);
     if (st == RAAS_OK) parts = PrefixParts{P.part, P.ml, P.nsplit, P.rows};
     return st;
@@ -325,7 +317,8 @@ raas_status raas_weight_step(raas_weight_cache* c, int32_t layer, const void* q,
     hipStream_t s = (hipStream_t)stream;
     WeightStepIO io{q, k_new, v_new, out, positions_out, weights_out, evicted_out, active, PrefixParts{}};
     if (prefix) {
-        st = step_prefix_parts(prefix, layer, q, c->cfg.batch, io.prefix, s);
+        double bytes;
+        st = step_prefix_parts(prefix, layer, q, c->cfg.batch, io.prefix, bytes, s);
         if (st != RAAS_OK) return st;
     }
     // What other layers, caches and pools have read since the layer's last step

@@ -10,7 +10,7 @@ d (3 d) sums round: a logit is off by dx = (d + 4) u X, ((3 d + 4) u X), X = sum
 itself. An output is off by rel A, A = sum_j a_j |v_j|. In a bf16 cache the two
 bf16 pieces of a probability leave 2^-15 of it (less than 2^-7 after the first, of
 which the second is off by half a step, 2^-8), and the output is rounded, 2^-8 of
-its size. In calls of more than 32 rows per KV head a probability of a bf16 cache is
+its size. In calls of more than 16 rows per KV head a probability of a bf16 cache is
 one fp16 instead, off by half a step, 2^-11 of it, or, below 2^-14 of a unit that
 is at most 2^-7 of the largest (2^-21 of it), by 2^-25 of that unit: 2^-32 of the
 largest; the values beside it are exact. In an fp32 cache three pieces leave nothing, and their 3 n sums round."""

@@ -238,7 +238,7 @@ class Model:
                     if seen is not None:
                         K, V = K[seen(b, last)], V[seen(b, last)]
                     heads = slice(h * G, (h + 1) * G)
-                    o, ob, l, lb = ref.attention(qn[b, i, heads], K, V, self.bf16, half=n * G > 32)
+                    o, ob, l, lb = ref.attention(qn[b, i, heads], K, V, self.bf16, half=n * G > 16)
                     _within(got[b, i, heads], o, ob, ("out", b, i, h))
                     _within(gl[b, i, heads], l, lb, ("lse", b, i, h))
         return out, lse
