@@ -71,9 +71,10 @@ __device__ __forceinline__ void load_query(const T* row, bool real, int a,
 // equally many blocks over the whole batch, so that ragged sequences load the
 // chip evenly: every workgroup finds its own from the lengths, which the host does
 // not know. Parts are cut so that about `target` workgroups come out, but of at
-// least `least` blocks, and at most kMaxQuantParts per tile.
+// least `least` blocks, of 8 where there would be more than 16 of them, and at most
+// kMaxQuantParts per tile; a tile of up to `whole` blocks is not cut.
 struct Cut {
-    int target, least;
+    int target, least, whole;
 };
 struct Work {
     int b, h, tile, tiles, part, parts;
@@ -122,10 +123,11 @@ __device__ __forceinline__ int chunk_of(const QuantView& L, const QuantAttention
         sizes_of(L, io, b, held, rows);
         cost += (float)blocks_of(L, io, held) * ((rows + ROWS - 1) / ROWS);
     }
-    return max(cut.least, (int)ceilf(wave_sum(cost) * L.nkv / cut.target));
+    return (int)ceilf(wave_sum(cost) * L.nkv / cut.target);
 }
-__device__ __forceinline__ int parts_of(int blocks, int chunk) {
-    return max(1, min(kMaxQuantParts, (blocks + chunk - 1) / chunk));
+__device__ __forceinline__ int parts_of(int blocks, int chunk, const Cut& cut) {
+    const int each = max(chunk, blocks > 16 * cut.least ? 8 : cut.least);
+    return blocks <= cut.whole ? 1 : min(kMaxQuantParts, (blocks + each - 1) / each);
 }
 
 // The work of workgroup `wg`, or false where there is less than the grid allows for.
@@ -138,7 +140,7 @@ __device__ __forceinline__ bool find_work(const QuantView& L, const QuantAttenti
     for (int b0 = 0; b0 < L.batch; b0 += 64) {
         int t0, r0;
         sizes_of(L, io, b0 + lane, t0, r0);
-        const int parts = parts_of(blocks_of(L, io, t0), chunk), n = L.nkv * tiles_of(r0) * parts, own = parts > 1 ? n : 0;
+        const int parts = parts_of(blocks_of(L, io, t0), chunk, cut), n = L.nkv * tiles_of(r0) * parts, own = parts > 1 ? n : 0;
         const int upto = scan_sum(n), split = scan_sum(own);
         const unsigned long long m = __ballot(wg < before + upto);
         if (m == 0ull) {
@@ -178,7 +180,7 @@ __device__ __forceinline__ void for_split_rows(const QuantView& L, const QuantAt
     for (int b0 = 0; b0 < L.batch; b0 += 64) {
         int t0, r0;
         sizes_of(L, io, b0 + lane, t0, r0);
-        const int parts = parts_of(blocks_of(L, io, t0), chunk), tiles = (r0 + ROWS - 1) / ROWS;
+        const int parts = parts_of(blocks_of(L, io, t0), chunk, cut), tiles = (r0 + ROWS - 1) / ROWS;
         const int n = parts > 1 ? L.nkv * r0 : 0, own = parts > 1 ? L.nkv * tiles * parts : 0;
         const int upto = scan_sum(n), split = scan_sum(own), all = before + __builtin_amdgcn_readlane(upto, 63);
         for (; i < all; i += step) {

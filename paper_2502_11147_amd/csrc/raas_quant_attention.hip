@@ -141,7 +141,14 @@ template <typename T, int KB, int VB, bool STREAM>
 constexpr int kStreamBlocks = STREAM && KB + VB == 8 && sizeof(T) == 2 ? 4 : 2;
 template <typename T, int KB, int VB, bool STREAM>
 constexpr int kStreamPerSimd = sizeof(T) == 4 ? 1 : kStreamBlocks<T, KB, VB, STREAM> == 4 ? 2 : 3;
-constexpr Cut kStreamCut = {256, 8};
+// Parts: of 8 KV heads with 30000 tokens in 64, 43 and 32 parts 17.9, 17.0 and 15.2 us:
+// publishing a part and joining it costs more than a workgroup's share of an even
+// load, once every compute unit has one. One sequence of 1000 tokens takes 8.2, 8.8
+// and 9.9 us in parts of 4, 8 and 16 blocks, of 4000 tokens 10.8 and 8.9 of 4 and 8
+// (a join has 16 parts on their way together). Publishing at all costs as much as
+// five turns: one sequence of 300 tokens takes 7.2 us in one part, 8.6 in two, of
+// 600 tokens 8.4 and 8.9.
+constexpr Cut kStreamCut = {256, 4, 20};
 
 template <typename T, int D, int KB, int VB, bool STREAM>
 __global__ __launch_bounds__(kStreamWaves * 64)

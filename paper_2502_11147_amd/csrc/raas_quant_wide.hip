@@ -20,7 +20,7 @@ template <typename T>
 constexpr int kRowTiles = sizeof(T) == 2 ? 2 : 1;
 template <typename T>
 constexpr int kWideRows = 16 * kRowTiles<T>;
-constexpr Cut kWideCut = {1024, 8};
+constexpr Cut kWideCut = {1024, 8, 8};
 
 // Beside a bf16 cache's values, probabilities are rounded to fp16 (half a step,
 // 2^-11 of themselves, an eighth of what the rounding of a bf16 output may be; in
@@ -268,7 +268,7 @@ template <typename T, int D, int KB, int VB>
 hipError_t launch(const QuantView& L, const QuantAttention& io, hipStream_t s) {
     const size_t grid = most_workgroups(kWideCut, kWideRows<T>, L.batch, io.queries, L.nkv, L.G);
     hipLaunchKernelGGL((k_quant_wide<T, D, KB, VB>), dim3((unsigned)grid), dim3(64), 0, s, L, io);
-    if (L.cap / kQuantBlock > kWideCut.least) {  // (else no part is cut)
+    if (L.cap / kQuantBlock > kWideCut.whole) {  // (else no tile is cut)
         const size_t rows = (size_t)L.batch * L.nkv * io.queries * L.G;
         hipLaunchKernelGGL((k_quant_join<T, D>), dim3((unsigned)std::min((rows + 3) / 4, (size_t)kJoinWorkgroups)),
                            dim3(256), 0, s, L, io);
