@@ -209,7 +209,11 @@ __device__ __forceinline__ void for_split_rows(const QuantView& L, const QuantAt
 // -inf, never NaN.
 constexpr float kSlack = 8.0f, kLowest = -1e30f;
 
-// Logits (unscaled) of a block's keys and RT tiles of 16 rows. A row of this lane's
+// Logits (unscaled) of a block's keys and RT tiles of 16 rows. (v_mfma_scale_f32_
+// 16x16x128_f8f6f4 takes keys of 4 bits as they are stored, beside a query as two e4m3
+// numbers, and saves the 36 conversions of a block; but its sums are off by up to
+// 1.3e-5 of the products' magnitudes, a hundred times what these are: a log-sum-exp
+// was off by 3e-4.) A row of this lane's
 // column sees tokens below lim[t] of the block; `masked`: some row does not see all.
 template <typename T, int D, int KB, int VB, int RT>
 __device__ __forceinline__ void block_logits(const Block<D, KB, VB>& blk, const u32x4 (&q)[RT][D / 32][kQueryPieces<T>],

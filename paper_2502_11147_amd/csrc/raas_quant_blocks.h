@@ -62,7 +62,12 @@ struct Format {
     static constexpr int VSHARE = kQuantGroup / VC;
 };
 
+// The scale operand of a conversion, whose exponent alone counts (its sign and
+// mantissa may be anything): of an exponent byte, and of byte j of four.
 __device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
+__device__ __forceinline__ uint32_t scale_bits(uint32_t four, int j) {
+    return j == 0 ? four << 23 : j == 1 ? four << 15 : j == 2 ? four << 7 : four >> 1;
+}
 
 template <bool NT>
 __device__ __forceinline__ u32x4 load16(const uint8_t* p) {
@@ -81,7 +86,7 @@ struct Keys {
         for (int p = 0; p < F::NKP; ++p) k[p] = load16<NT>(rec + 1024 * p + 16 * lane);
         ke = *reinterpret_cast<const uint16_t*>(rec + F::KEXP + (F::kgroup(lane >> 4) * 16 + (lane & 15)) * 2);
     }
-    __device__ __forceinline__ float key_scale(int q) const { return scale_of(q ? ke >> 8 : ke & 255u); }
+    __device__ __forceinline__ float key_scale(int q) const { return __uint_as_float(scale_bits(ke, q)); }
     // Channels 8 ks .. 8 ks + 7 of this lane's key of tile q, as bf16.
     __device__ __forceinline__ u32x4 key(int q, int ks, float scale) const {
         u32x4 r;
@@ -141,8 +146,10 @@ struct Values {
             v[0][j >> 1] = j & 1 ? (x & 0xFFFFu) | c[0] << 16 : (x & 0xFFFF0000u) | (c[0] & 0xFFFFu);
         }
     }
-    __device__ __forceinline__ uint32_t exponent(int j) const { return ve[j >> 2] >> (8 * (j & 3)) & 255u; }
-    __device__ __forceinline__ float value_scale(int j) const { return scale_of(exponent(j)); }
+    // times 2^by
+    __device__ __forceinline__ float value_scale(int j, int by = 0) const {
+        return __uint_as_float(scale_bits(ve[j >> 2], j & 3) + ((uint32_t)by << 23));
+    }
     // Channels 2 M and 2 M + 1 of this lane's values of token j, as bf16 or (HALF) fp16.
     template <int M, bool HALF = false>
     __device__ __forceinline__ uint32_t value2(int j, float scale) const {

@@ -74,7 +74,7 @@ __device__ __forceinline__ void attend_half(const Block<D, KB, VB>& blk, const u
     }
     float scale[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) scale[j] = scale_of(blk.exponent(j) + 127 - Half<VB>::kUnit);
+    for (int j = 0; j < 8; ++j) scale[j] = blk.value_scale(j, 127 - Half<VB>::kUnit);
     auto two = [&](auto m) {
         constexpr int M = decltype(m)::value;
         u32x4 even, odd;

@@ -462,6 +462,31 @@ def test_values_of_any_scale(queries, bits, d):
 
 
 @gpu
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("queries", [1, 40])
+def test_queries_of_any_scale(queries, bits):
+    """Groups of a query far larger and smaller than others, zeros, outliers among small ones."""
+    import torch
+
+    m = Model([0, 0, 0], 4, 2, 128, bits, page=32, width=4, max_queries=queries)
+    m.write([97, 33, 64])
+    plain = m.query
+
+    def query(*lead):
+        q = plain(*lead)[1]
+        q[0, ..., :32] *= 2.0 ** -9
+        q[0, ..., 64] *= 2.0 ** 5
+        q[1, ..., 3::8] = 0
+        q[1, ..., 96:] *= 2.0 ** -30
+        q[2, ..., 1:] *= 2.0 ** -np.arange(127)
+        t = _dev(q.astype(np.float32), torch.bfloat16)
+        return t, _np(t)
+
+    m.query = query
+    m.attend(queries)
+
+
+@gpu
 def test_one_sequence_of_many_heads():
     m = Model([3000], 32, 8, 128, (4, 4), page=256, max_queries=8)
     m.attend(1)
