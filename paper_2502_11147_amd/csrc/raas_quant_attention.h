@@ -311,6 +311,11 @@ __device__ __forceinline__ void attend_block(const Block<D, KB, VB>& blk, const 
     }
 }
 
+// Natural logarithm of sum 2^m; -inf of none.
+__device__ __forceinline__ float natural_log(float m, float sum) {
+    return sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+}
+
 // A row's place in out and lse.
 __device__ __forceinline__ size_t row_at(const QuantView& L, const QuantAttention& io, const Work& w, int row) {
     const int i = row / L.G, g = row - i * L.G;

@@ -5,7 +5,8 @@
 // Codes become bf16 in registers (exactly: at most four significant bits times a
 // power of two) and the products run on the matrix cores with fp32 sums.
 // Probabilities are fp32 and enter as the sum of two bf16; queries of an fp32
-// cache, and its probabilities, as that of three, which is exact.
+// cache, and its probabilities, as that of three, which is exact. Here units of few
+// rows; raas_quant_wide.hip takes more.
 #include <math.h>
 
 #include <algorithm>
@@ -41,11 +42,11 @@ __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAtten
         const float2 x = lane < parts ? part_ml(lane) : none, y = lane + 64 < parts ? part_ml(lane + 64) : none;
         const float M = fmaxf(wave_max(fmaxf(x.x, y.x)), -1e30f);
         const float ex = __builtin_amdgcn_exp2f(x.x - M), ey = __builtin_amdgcn_exp2f(y.x - M);
-        const float Z = wave_sum(x.y * ex + y.y * ey), rz = Z > 0.0f ? 1.0f / Z : 0.0f;
+        const float Z = wave_sum(x.y * ex + y.y * ey), rz = Z == 0.0f ? 0.0f : 1.0f / Z;
         if (lane < parts) s_w[lane][row] = ex * rz;
         if (lane + 64 < parts) s_w[lane + 64][row] = ey * rz;
         if (io.lse != nullptr && lane == 0)
-            io.lse[to(row)] = Z > 0.0f ? (M + __builtin_amdgcn_logf(Z)) * 0.69314718055994530942f : -INFINITY;
+            io.lse[to(row)] = natural_log(M, Z);
     }
     __syncthreads();
     typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
@@ -57,11 +58,9 @@ __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAtten
             for (int s0 = 0; s0 < n; s0 += AHEAD) {
                 f32x4 y[AHEAD];
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k)
-                    y[k] = value(min(s0 + k, n - 1));
+                for (int k = 0; k < AHEAD; ++k) y[k] = value(min(s0 + k, n - 1));
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k)
-                    x += y[k] * (s0 + k < n ? s_w[w0 + s0 + k][row] : 0.0f);
+                for (int k = 0; k < AHEAD; ++k) x += y[k] * (s0 + k < n ? s_w[w0 + s0 + k][row] : 0.0f);
             }
         };
         add(nsrc, 0, [&](int k) { return o(k, row, c); });
@@ -127,11 +126,13 @@ __device__ __forceinline__ void take_token(const QuantAttention& io, Block<D, KB
 }
 
 // ---------------------------------------------------------------------------
-// Few rows per unit: a workgroup's wavefronts take the blocks of its part in
+// Up to 16 rows per unit: a workgroup's wavefronts take the blocks of its part in
 // turn, a block on its way while the one before it is attended to, join in LDS,
-// and write the outputs, or publish the part: the last of a tile's parts to end
-// joins them all. Pages of a wavefront's next 64 blocks lie in its lanes.
-constexpr int kStreamWaves = 4;
+// and write the outputs, or publish the part: the last of a unit's parts to end
+// joins them all. Pages of a wavefront's next 64 blocks lie in its lanes. Bound by
+// memory, 4.25 or 8.25 bits a value (128 sequences of 8192 tokens in 4 bits 6.3 TB/s);
+// small calls by the chain of lengths, table, block, join (6 us, 8 with parts).
+constexpr int kStreamWaves = 4, kStreamRows = 16;
 // Blocks of a wavefront on their way or in use, and wavefronts per SIMD. A layer
 // that streams from memory in 4 bits (128 sequences of 8192 tokens) takes 221 us
 // with two and three, 198 with non-temporal loads, 181 with four and two besides;
@@ -155,28 +156,22 @@ __global__ __launch_bounds__(kStreamWaves * 64)
 __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_quant_stream(QuantView L,
                                                                                             QuantAttention io) {
     using F = Format<D, KB, VB>;
-    constexpr int NW = kStreamWaves, RT = 1, TR = 16, NB = kStreamBlocks<T, KB, VB, STREAM>;
+    constexpr int NW = kStreamWaves, NB = kStreamBlocks<T, KB, VB, STREAM>;
     __shared__ __align__(16) float s_o[NW][16][D + 4];
     __shared__ float s_m[NW][16], s_l[NW][16], s_w[kFinishSources][16];
     const int tid = threadIdx.x, lane = tid & 63, wv = wave_of(tid), a = lane >> 4, col = lane & 15;
     Work w;
-    if (!find_work<TR>(L, io, kStreamCut, lane, blockIdx.x, w)) return;
-    const int rows = min(TR, w.rows - w.tile * TR), count = w.rows / L.G;
+    if (!find_work<kStreamRows>(L, io, kStreamCut, lane, blockIdx.x, w)) return;
+    const int first = w.tile * kStreamRows, rows = min(kStreamRows, w.rows - first), count = w.rows / L.G;
     // a row sees the tokens up to its own: query i of `count` lies at tokens - count + i
     auto limit = [&](int row) { return w.tokens - count + 1 + row / L.G; };
-    int lim[RT];
-    u32x4 q[RT][F::KS][kQueryPieces<T>];
-    Softmax<D> s[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int row = w.tile * TR + 16 * t + col;
-        const bool real = 16 * t + col < rows;
-        load_query<T, D>((const T*)io.q + row_at(L, io, w, row) * D, real, a, q[t]);
-        lim[t] = real ? limit(row) : 0;
-        s[t].clear();
-        s[t].m = kLowest;
-    }
-    const int first = w.tile * TR, most = max(0, limit(first + rows - 1)), least = limit(first);
+    u32x4 q[1][F::KS][kQueryPieces<T>];
+    load_query<T, D>((const T*)io.q + row_at(L, io, w, first + col) * D, col < rows, a, q[0]);
+    const int lim = col < rows ? limit(first + col) : 0;
+    Softmax<D> s[1];
+    s[0].clear();
+    s[0].m = kLowest;
+    const int most = max(0, limit(first + rows - 1)), least = limit(first);
     const int nb = blocks_of(most), per = (nb + w.parts - 1) / w.parts;
     const int lo = min(nb, w.part * per), hi = min(nb, lo + per);
     const int32_t* table = L.table + (size_t)w.b * L.width;
@@ -200,10 +195,8 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_q
     };
     auto attend = [&](int b, Block<D, KB, VB>& blk) {
         const int t0 = b * kQuantBlock;
-        int l[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) l[t] = lim[t] - t0;
-        attend_block<T, D, KB, VB, RT>(blk, q, t0 + kQuantBlock > least, l, a, io.scale_log2, s);
+        const int l[1] = {lim - t0};
+        attend_block<T, D, KB, VB, 1>(blk, q, t0 + kQuantBlock > least, l, a, io.scale_log2, s);
     };
     if (turns > 0) {
         fetch(0, Int<0>());
@@ -242,72 +235,56 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_q
             attend(b, blk);
         }
     }
-    const bool split = w.parts > 1;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int here = min(16, rows - 16 * t);
-        if (here <= 0) break;
-        const float l = sum_groups(s[t].l);
-        if (a == 0) {
-            s_m[wv][col] = s[t].m;
-            s_l[wv][col] = l;
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float* to = &s_o[wv][col][(4 * a + r) * F::VC];
-#pragma unroll
-            for (int ct = 0; ct < F::VC; ct += 4)
-                *reinterpret_cast<f32x4*>(to + ct) =
-                    f32x4{s[t].o[ct][r], s[t].o[ct + 1][r], s[t].o[ct + 2][r], s[t].o[ct + 3][r]};
-        }
-        __syncthreads();
-        auto ml = [&](int k, int row) { return make_float2(s_m[k][row], s_l[k][row]); };
-        if (!split) {
-            finish_rows<T, D, NW>(L, io, w, first + 16 * t, here, tid, NW, s_w, ml,
-                                  [&](int k, int row, int c) { return *reinterpret_cast<const f32x4*>(&s_o[k][row][c]); });
-            continue;
-        }
-        const size_t slot = (size_t)(w.slot + w.part) * TR + 16 * t;
-        for (int e = tid; e < here * (D / 4); e += NW * 64) {
-            const int row = e / (D / 4), c = e % (D / 4) * 4;
-            float M = kLowest, z = 0.0f;
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < NW; ++k) M = fmaxf(M, s_m[k][row]);
-#pragma unroll
-            for (int k = 0; k < NW; ++k) {
-                const float share = __builtin_amdgcn_exp2f(s_m[k][row] - M);
-                x += *reinterpret_cast<const f32x4*>(&s_o[k][row][c]) * share;
-                z = __builtin_fmaf(s_l[k][row], share, z);
-            }
-            publish4(io.part + (slot + row) * D + c, x);
-            if (c == 0) {
-                publish(io.ml + 2 * (slot + row), M);
-                publish(io.ml + 2 * (slot + row) + 1, z);
-            }
-        }
-        __syncthreads();
+    const float sum = sum_groups(s[0].l);
+    if (a == 0) {
+        s_m[wv][col] = s[0].m;
+        s_l[wv][col] = sum;
     }
-    if (!split) return;
-    const int tiles = (io.queries * L.G + TR - 1) / TR;  // (of the call: the counters' layout)
-    if (!arrive_last(io.arrived + ((size_t)w.b * L.nkv + w.h) * tiles + w.tile, w.parts)) return;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int here = min(16, rows - 16 * t);
-        if (here <= 0) break;
-        auto at = [&](int k, int row) { return (size_t)(w.slot + k) * TR + 16 * t + row; };
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int ct = 0; ct < F::VC; ct += 4)
+            *reinterpret_cast<f32x4*>(&s_o[wv][col][(4 * a + r) * F::VC + ct]) =
+                f32x4{s[0].o[ct][r], s[0].o[ct + 1][r], s[0].o[ct + 2][r], s[0].o[ct + 3][r]};
+    __syncthreads();
+    auto o = [&](int k, int row, int c) { return *reinterpret_cast<const f32x4*>(&s_o[k][row][c]); };
+    if (w.parts == 1) {
         finish_rows<T, D, NW>(
-            L, io, w, first + 16 * t, here, tid, w.parts, s_w,
-            [&](int k, int row) {
-                return make_float2(published(io.ml + 2 * at(k, row)), published(io.ml + 2 * at(k, row) + 1));
-            },
-            [&](int k, int row, int c) { return published4(io.part + at(k, row) * D + c); });
+            L, io, w, first, rows, tid, NW, s_w, [&](int k, int row) { return make_float2(s_m[k][row], s_l[k][row]); }, o);
+        return;
     }
+    const size_t slot = (size_t)(w.slot + w.part) * kStreamRows;
+    for (int e = tid; e < rows * (D / 4); e += NW * 64) {
+        const int row = e / (D / 4), c = e % (D / 4) * 4;
+        float M = kLowest, z = 0.0f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NW; ++k) M = fmaxf(M, s_m[k][row]);
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            const float share = __builtin_amdgcn_exp2f(s_m[k][row] - M);
+            x += o(k, row, c) * share;
+            z = __builtin_fmaf(s_l[k][row], share, z);
+        }
+        publish4(io.part + (slot + row) * D + c, x);
+        if (c == 0) {
+            publish(io.ml + 2 * (slot + row), M);
+            publish(io.ml + 2 * (slot + row) + 1, z);
+        }
+    }
+    if (!arrive_last(io.arrived + (size_t)w.b * L.nkv + w.h, w.parts)) return;  // (a unit's rows are one tile)
+    auto at = [&](int k, int row) { return (size_t)(w.slot + k) * kStreamRows + row; };
+    finish_rows<T, D, NW>(
+        L, io, w, first, rows, tid, w.parts, s_w,
+        [&](int k, int row) {
+            return make_float2(published(io.ml + 2 * at(k, row)), published(io.ml + 2 * at(k, row) + 1));
+        },
+        [&](int k, int row, int c) { return published4(io.part + at(k, row) * D + c); });
 }
 
 template <typename T, int D, int KB, int VB>
 hipError_t launch(const QuantView& L, const QuantAttention& io, bool stream, hipStream_t s) {
-    const size_t grid = most_workgroups(kStreamCut, 16, L.batch, io.queries, L.nkv, L.G);
+    const size_t grid = most_workgroups(kStreamCut, kStreamRows, L.batch, io.queries, L.nkv, L.G);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kStreamWaves * 64), 0, s, L, io);
     };
@@ -316,21 +293,15 @@ hipError_t launch(const QuantView& L, const QuantAttention& io, bool stream, hip
     return hipGetLastError();
 }
 
-// Most rows per unit that the kernel for few takes.
-constexpr int kStreamRows = 16;
-
 }  // namespace
 
 QuantScratch quant_scratch(int batch, int queries, int nkv, int G) {
     // Every split tile has at least two parts of `chunk` blocks but for the last, and
     // all blocks together are at most target * chunk: at most 2 target slots.
-    auto tiles = [&](int q, int r) { return (size_t)batch * nkv * ((q * G + r - 1) / r); };
-    QuantScratch x = quant_wide_scratch(batch, queries, nkv, G);
-    const int few = std::min(queries, kStreamRows / G);
-    const size_t t = tiles(few, 16);
-    x.rows = std::max(x.rows, std::min((size_t)2 * kStreamCut.target, t * kMaxQuantParts) * 16);
-    x.arrivals = t;
-    return x;
+    // (A unit's rows are one tile here.)
+    const size_t units = (size_t)batch * nkv;
+    const size_t rows = std::min((size_t)2 * kStreamCut.target, units * kMaxQuantParts) * kStreamRows;
+    return {std::max(rows, quant_wide_scratch_rows(batch, queries, nkv, G)), units};
 }
 
 hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, bool stream, hipStream_t s) {

@@ -56,8 +56,7 @@ struct QuantAttention {
     PrefixParts prefix;    // n = 0: none (a step's only)
     float scale_log2;
     // scratch: unnormalised outputs, maxima (base 2) and sums of tiles that are
-    // split, a slot of a tile's rows per workgroup; arrivals per unit and tile, zero
-    // between launches
+    // split, a slot of a tile's rows per workgroup; arrivals per unit, zero between launches
     float* part;
     float* ml;
     int32_t* arrived;
@@ -71,7 +70,7 @@ struct QuantScratch {
     size_t arrivals;  // of arrived
 };
 QuantScratch quant_scratch(int batch, int queries, int nkv, int G);
-QuantScratch quant_wide_scratch(int batch, int queries, int nkv, int G);
+size_t quant_wide_scratch_rows(int batch, int queries, int nkv, int G);
 // stream: codes are read with non-temporal loads
 hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, bool stream, hipStream_t s);
 // Its kernels for many rows per unit.

@@ -20,8 +20,8 @@ struct Span {
     int shift, page;
     __device__ __forceinline__ bool find(const QuantView& L, const QuantCopy& io, int b, int nth) {
         const int start = io.start[b], count = min(io.count != nullptr ? io.count[b] : io.stride, io.stride);
-        if (start < 0 || count <= 0) return false;
-        const int end = min((long long)start + count, (long long)L.cap);
+        if (start < 0 || start >= L.cap || count <= 0) return false;
+        const int end = min(start + count, L.cap);  // (both below 2^21)
         blk = start / kQuantBlock + nth;
         const int t0 = blk * kQuantBlock;
         lo = max(start - t0, 0);

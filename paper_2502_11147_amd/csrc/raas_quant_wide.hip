@@ -201,9 +201,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2))) void
             continue;
         }
         const size_t at = row_at(L, io, w, row);
-        const float rl = l > 0.0f ? unit / l : 0.0f;
-        if (io.lse != nullptr && a == 0)
-            io.lse[at] = l > 0.0f ? (s[t].m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+        const float rl = l == 0.0f ? 0.0f : unit / l;
+        if (io.lse != nullptr && a == 0) io.lse[at] = natural_log(s[t].m, l);
         typedef T Tv __attribute__((ext_vector_type(F::VC), aligned(sizeof(T))));
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -231,7 +230,7 @@ __global__ __launch_bounds__(256) void k_quant_join(QuantView L, QuantAttention 
         static_assert(kMaxQuantParts <= 64, "");
         if (lane < w.parts) ml = *reinterpret_cast<const float2*>(io.ml + 2 * (at + (size_t)lane * TR));
         const float M = wave_max(ml.x), e = __builtin_amdgcn_exp2f(ml.x - M), Z = wave_sum(ml.y * e);
-        const float share = Z > 0.0f ? e / Z : 0.0f;
+        const float share = Z == 0.0f ? 0.0f : e / Z;
         const int c = lane % LANES * 4;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int p0 = 0; p0 < w.parts; p0 += 8 * AT) {
@@ -259,8 +258,7 @@ __global__ __launch_bounds__(256) void k_quant_join(QuantView L, QuantAttention 
             for (int k = 0; k < 4; ++k) o[k] = from_f<T>(x[k]);
             *reinterpret_cast<T4*>((T*)io.out + to * D + c) = o;
         }
-        if (io.lse != nullptr && lane == 0)
-            io.lse[to] = Z > 0.0f ? (M + __builtin_amdgcn_logf(Z)) * 0.69314718055994530942f : -INFINITY;
+        if (io.lse != nullptr && lane == 0) io.lse[to] = natural_log(M, Z);
     });
 }
 
@@ -278,13 +276,13 @@ hipError_t launch(const QuantView& L, const QuantAttention& io, hipStream_t s) {
 
 }  // namespace
 
-QuantScratch quant_wide_scratch(int batch, int queries, int nkv, int G) {
+size_t quant_wide_scratch_rows(int batch, int queries, int nkv, int G) {
     size_t rows = 0;
     for (int tile : {kWideRows<uint16_t>, kWideRows<float>}) {
         const size_t tiles = (size_t)batch * nkv * ((queries * G + tile - 1) / tile);
         rows = std::max(rows, std::min((size_t)2 * kWideCut.target, tiles * kMaxQuantParts) * tile);
     }
-    return {rows, 0};
+    return rows;
 }
 
 hipError_t launch_quant_wide(const QuantView& L, bool bf16, const QuantAttention& io, hipStream_t s) {

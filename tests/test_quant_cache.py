@@ -487,6 +487,47 @@ def test_queries_of_any_scale(queries, bits):
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("queries", [1, 30])
+def test_nan_stays_visible(queries, bits, d):
+    """A NaN among the values reaches the outputs of its channels, one among the keys those of
+    every channel and the log-sum-exp; other KV heads and sequences have none."""
+    import torch
+
+    m = Model([0, 0, 0], 6, 3, d, bits, page=32, width=4, max_queries=queries)
+    x = m.rng.standard_normal((2, 3, 3, 100, d)).astype(np.float32)
+    x[0, 0, 1, 5, 3], x[1, 1, 2, 40, d - 1] = np.nan, np.nan
+    m.cache.write(0, _dev(x[0], m.dt), _dev(x[1], m.dt), m.table, _ints([0] * 3))
+    q, _ = m.query(3, queries)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")
+    m.cache.attend(0, q, out, m.table, _ints([100] * 3), None, lse)
+    want, log = np.zeros(tuple(q.shape), bool), np.zeros(tuple(lse.shape), bool)
+    want[0, :, 2:4], log[0, :, 2:4] = True, True
+    want[1, :, 4:6, d - 32:] = True
+    assert np.array_equal(np.isnan(_np(out)), want) and np.array_equal(np.isnan(_np(lse)), log)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("queries", [1, 4, 24])
+def test_outputs_at_any_alignment(queries, dtype):
+    """Outputs one element into their memory; the elements around them stay."""
+    import torch
+
+    m = Model([700, 65, 0], 4, 2, 128, (8, 4), dtype, page=64, max_queries=queries)
+    q, _ = m.query(3, queries)
+    want, lse = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")
+    m.cache.attend(0, q, want, m.table, _ints(m.lens()), None, lse)
+    mem, lmem = torch.full((q.numel() + 2,), 5.0, dtype=m.dt, device="cuda"), torch.full((lse.numel() + 2,), 5.0, device="cuda")
+    out, l = mem[1:-1].view(q.shape), lmem[1:-1].view(lse.shape)
+    m.cache.attend(0, q, out, m.table, _ints(m.lens()), None, l)
+    assert torch.equal(out, want) and torch.equal(l, lse)
+    for x in (mem, lmem):
+        assert x[0] == 5.0 and x[-1] == 5.0
+
+
+@gpu
 def test_one_sequence_of_many_heads():
     m = Model([3000], 32, 8, 128, (4, 4), page=256, max_queries=8)
     m.attend(1)
