@@ -21,7 +21,8 @@
 // the same D / 16 consecutive channels of the values. One record:
 //   key codes    piece p of lane l at 1024 p + 16 l; a lane's bytes in order:
 //                tile q < 2, channels D/4 a .. of token 8 (i/4) + 4 q + i % 4
-//   value codes  likewise; token 8 a + j, j < 8, channels D/16 i ..
+//   value codes  likewise: the lower half of channels D/16 i .. of tokens 8 a + j,
+//                j < 8, then the upper half
 //   exponents    of keys: [group][i][q] bytes; of values: [a][group][j]
 #pragma once
 
@@ -49,6 +50,7 @@ struct Format {
     static constexpr int NG = D / kQuantGroup;   // groups of a token
     static constexpr int KD = KC * KB / 32;      // dwords of a lane's key (one tile)
     static constexpr int VBYTES = VC * VB / 8;   // bytes of a lane's values (one token)
+    static constexpr int VHALF = VBYTES / 2;     // of half of them
     static constexpr int NKP = 2 * KD / 4;       // 16-byte pieces of a lane's keys
     static constexpr int NVP = 8 * VBYTES / 16;  // and of its values
     static constexpr int VALUES = NKP * 1024;    // offsets in a record
@@ -67,6 +69,38 @@ struct Format {
 __device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
 __device__ __forceinline__ uint32_t scale_bits(uint32_t four, int j) {
     return j == 0 ? four << 23 : j == 1 ? four << 15 : j == 2 ? four << 7 : four >> 1;
+}
+
+// Two codes, from byte `at` of a dword (a constant once loops are unrolled), as bf16 or (HALF) fp16.
+template <int BITS, bool HALF>
+__device__ __forceinline__ uint32_t two_values(uint32_t x, int at, float scale) {
+    auto cast = [](auto y) { return __builtin_bit_cast(uint32_t, y); };
+    if constexpr (BITS == 8) {
+        if constexpr (HALF)
+            return at ? cast(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, scale, true))
+                      : cast(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, scale, false));
+        else
+            return at ? cast(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))
+                      : cast(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false));
+    } else if constexpr (HALF) {
+        return at == 0   ? cast(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, 0))
+               : at == 1 ? cast(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, 1))
+               : at == 2 ? cast(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, 2))
+                         : cast(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, 3));
+    } else {
+        return at == 0   ? cast(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0))
+               : at == 1 ? cast(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1))
+               : at == 2 ? cast(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2))
+                         : cast(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3));
+    }
+}
+// Eight codes, in BITS / 4 dwords, as an operand of bf16.
+template <int BITS>
+__device__ __forceinline__ u32x4 eight_keys(const uint32_t* x, float scale) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = two_values<BITS, false>(x[BITS == 8 ? i >> 1 : 0], BITS == 8 ? 2 * (i & 1) : i, scale);
+    return r;
 }
 
 template <bool NT>
@@ -89,23 +123,9 @@ struct Keys {
     __device__ __forceinline__ float key_scale(int q) const { return __uint_as_float(scale_bits(ke, q)); }
     // Channels 8 ks .. 8 ks + 7 of this lane's key of tile q, as bf16.
     __device__ __forceinline__ u32x4 key(int q, int ks, float scale) const {
-        u32x4 r;
         const int at = (q * F::KS + ks) * (KB / 4);
-        if constexpr (KB == 4) {
-            const uint32_t x = k[at >> 2][at & 3];
-            r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0));
-            r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1));
-            r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2));
-            r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3));
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t x = k[(at + h) >> 2][(at + h) & 3];
-                r[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false));
-                r[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true));
-            }
-        }
-        return r;
+        const uint32_t x[2] = {k[at >> 2][at & 3], k[(at + KB / 8) >> 2][(at + KB / 8) & 3]};
+        return eight_keys<KB>(x, scale);
     }
 };
 
@@ -136,14 +156,18 @@ struct Values {
     }
     // Token j's codes of this lane's values (VBYTES of them).
     __device__ __forceinline__ void set_value(int j, u32x2 c) {
-        if constexpr (F::VBYTES == 8) {
-            v[j >> 1][2 * (j & 1)] = c[0];
-            v[j >> 1][2 * (j & 1) + 1] = c[1];
-        } else if constexpr (F::VBYTES == 4) {
+        if constexpr (F::VHALF == 4) {
             v[j >> 2][j & 3] = c[0];
+            v[2 + (j >> 2)][j & 3] = c[1];
         } else {
-            const uint32_t x = v[0][j >> 1];
-            v[0][j >> 1] = j & 1 ? (x & 0xFFFFu) | c[0] << 16 : (x & 0xFFFF0000u) | (c[0] & 0xFFFFu);
+            constexpr int BITS = 8 * F::VHALF, PER = 32 / BITS;  // tokens of a dword
+            constexpr uint32_t ONES = (1u << BITS) - 1u;
+            const int sh = BITS * (j % PER);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = h * (8 / PER) + j / PER;
+                v[at >> 2][at & 3] = (v[at >> 2][at & 3] & ~(ONES << sh)) | (c[0] >> (BITS * h) & ONES) << sh;
+            }
         }
     }
     // times 2^by
@@ -153,25 +177,9 @@ struct Values {
     // Channels 2 M and 2 M + 1 of this lane's values of token j, as bf16 or (HALF) fp16.
     template <int M, bool HALF = false>
     __device__ __forceinline__ uint32_t value2(int j, float scale) const {
-        if constexpr (VB == 4) {
-            auto byte = [&](uint32_t x, auto n) {
-                if constexpr (HALF)
-                    return __builtin_bit_cast(uint32_t,
-                                              __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(x, scale, decltype(n)::value));
-                else
-                    return __builtin_bit_cast(uint32_t,
-                                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, decltype(n)::value));
-            };
-            if constexpr (D == 128) return byte(v[j >> 2][j & 3], Int<M>());
-            else return j & 1 ? byte(v[0][j >> 1], Int<(M & 1) + 2>()) : byte(v[0][j >> 1], Int<M & 1>());
-        } else {
-            const int at = D == 128 ? 2 * j + M / 2 : j;
-            const uint32_t x = v[at >> 2][at & 3];
-            if constexpr (HALF)
-                return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, scale, (M & 1) != 0));
-            else
-                return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, (M & 1) != 0));
-        }
+        constexpr int IN_HALF = F::VC / 4;  // pairs of channels of a half
+        const int at = (M / IN_HALF) * 8 * F::VHALF + j * F::VHALF + M % IN_HALF * (VB / 4);
+        return two_values<VB, HALF>(v[at >> 4][at >> 2 & 3], at & 3, scale);
     }
     // All of this lane's values of token j.
     __device__ __forceinline__ void value_row(int j, uint32_t (&x)[F::VC / 2]) const {
@@ -318,11 +326,14 @@ __device__ __forceinline__ uint32_t encode_value(const T* row, int i, u32x2& cod
 template <int D, int KB, int VB>
 __device__ __forceinline__ void store_value(uint8_t* rec, int lane, int j, const u32x2& code) {
     using F = Format<D, KB, VB>;
-    const int at = j * F::VBYTES;
-    uint8_t* to = rec + F::VALUES + 1024 * (at / 16) + 16 * lane + at % 16;
-    if constexpr (F::VBYTES == 8) *reinterpret_cast<u32x2*>(to) = code;
-    else if constexpr (F::VBYTES == 4) *reinterpret_cast<uint32_t*>(to) = code[0];
-    else *reinterpret_cast<uint16_t*>(to) = (uint16_t)code[0];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = (8 * h + j) * F::VHALF;
+        uint8_t* to = rec + F::VALUES + 1024 * (at / 16) + 16 * lane + at % 16;
+        if constexpr (F::VHALF == 4) *reinterpret_cast<uint32_t*>(to) = code[h];
+        else if constexpr (F::VHALF == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)(code[0] >> (16 * h));
+        else *to = (uint8_t)(code[0] >> (8 * h));
+    }
 }
 
 // N bf16 values, in dwords, to a caller's tensor of T.
