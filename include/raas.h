@@ -440,8 +440,9 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
  * A page holds page_size tokens of every KV head of a layer. Calls name the pages
  * of their sequences in `table`, DEVICE int32 [batch][table_width]: token t of
  * sequence b lies in page table[b][t / page_size], one of 0 .. n_pages - 1; every
- * layer has pages of its own under the same numbers. Sequences may share pages that
- * none of them writes. Tokens whose entry is no page, or that lie past the table's
+ * layer has pages of its own under the same numbers. A page may stand in a table
+ * more than once (sequences that share a prompt) if the call writes none of its
+ * tokens. Tokens whose entry is no page, or that lie past the table's
  * row, are neither written, read nor attended to. Tokens that were never written
  * hold anything. Table, lengths and counts are read when the call runs, so that
  * calls may be captured into a HIP graph: a replay works on what they hold then.

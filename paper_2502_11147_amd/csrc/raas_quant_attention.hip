@@ -50,17 +50,23 @@ __device__ __forceinline__ void finish_rows(const QuantView& L, const QuantAtten
     }
     __syncthreads();
     typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    constexpr int AHEAD = 16;  // reads on their way together
     for (int e = tid; e < rows * (D / 4); e += NW * 64) {
         const int row = e / (D / 4), c = e % (D / 4) * 4;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        // up to 16 reads on their way together; those of the last turn past the end are the last part's again
         auto add = [&](int n, int w0, auto value) {
-            for (int s0 = 0; s0 < n; s0 += AHEAD) {
+            auto turn = [&](auto ahead, int s0) {
+                constexpr int AHEAD = decltype(ahead)::value;
                 f32x4 y[AHEAD];
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) y[k] = value(min(s0 + k, n - 1));
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) x += y[k] * (s0 + k < n ? s_w[w0 + s0 + k][row] : 0.0f);
+            };
+            for (int s0 = 0; s0 < n; s0 += 16) {
+                if (n - s0 > 8) turn(Int<16>(), s0);
+                else if (n - s0 > 4) turn(Int<8>(), s0);
+                else turn(Int<4>(), s0);
             }
         };
         add(nsrc, 0, [&](int k) { return o(k, row, c); });

@@ -15,6 +15,10 @@ using namespace qnt;
 // 512 rows of four long prompts took 579 us against 632 then, but a prompt of 4096
 // tokens 179 against 168, 256 tokens behind 1000 41 against 35: reading it back, and
 // a barrier for every two blocks, took most of what it saved.)
+// Bound by vector instructions (active 70 % of the cycles) and products (39 %), which
+// two wavefronts per SIMD hardly overlap: 512 rows of four prompts of 16384 tokens
+// take 600 us, 896 TFLOP/s. A third wavefront, for which the query is read from LDS
+// anew and a block lies in registers only once, made it 699.
 constexpr int kWideRows = 32;
 constexpr Cut kWideCut = {1024, 8, 8};
 

@@ -835,3 +835,30 @@ def test_together(dtype):
     m.attend(20, counts=[0, 20, 0])
     m.step()
     m.check_held()
+
+
+@gpu
+def test_readme_example():
+    """The README's run, as it stands there."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        (code,) = [b.split("```")[0] for b in f.read().split("```python\n")[1:] if "QuantCache" in b]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    mk = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()
+    B, n, counts = 3, 100, [100, 1, 64]
+    x = dict(raas=raas, k_piece=mk(B, 8, n, 128), v_piece=mk(B, 8, n, 128), q_piece=mk(B, n, 32, 128), q=mk(B, 32, 128),
+             k_new=mk(B, 8, 128), v_new=mk(B, 8, 128), out=mk(B, 32, 128), o_piece=mk(B, n, 32, 128), start=_ints([0] * B),
+             counts=_ints(counts), table=torch.arange(2 * B, dtype=torch.int32, device="cuda").view(B, 2))
+    exec(code, x)
+    for b, c in enumerate(counts):
+        for h in (0, 7):
+            heads = slice(4 * h, 4 * h + 4)
+            K, V = (np.concatenate([ref.held(_np(x[p])[b, h, :c], 4), ref.held(_np(x[t])[b, h], 4)[None]])
+                    for p, t in (("k_piece", "k_new"), ("v_piece", "v_new")))
+            o, bound, _, _ = ref.attention(_np(x["q"])[b, heads], K, V, True)
+            _within(_np(x["out"])[b, heads], o, bound, ("step", b, h))
+            o, bound, _, _ = ref.attention(_np(x["q_piece"])[b, c - 1, heads], K[:-1], V[:-1], True, half=True)
+            _within(_np(x["o_piece"])[b, c - 1, heads], o, bound, ("piece", b, h))
