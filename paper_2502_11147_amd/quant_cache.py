@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import _check
+from . import _check, _torch, load_library
 from .weight_cache import SharedPrefix, _dtype_code, _Handle, _stream
 
 
@@ -33,13 +33,16 @@ class QuantCache(_Handle):
         self.n_layers, self.n_q_heads, self.n_kv_heads, self.head_dim = n_layers, n_q_heads, n_kv_heads, head_dim
         self.n_pages, self.page_size, self.max_batch, self.max_queries = n_pages, page_size, max_batch, max_queries
         self.key_bits, self.value_bits = key_bits, value_bits
+        self._write, self._read = (getattr(load_library(), "raas_quant_" + x) for x in ("write", "read"))
+        self._current_stream = _torch().cuda.current_stream
         super().__init__("raas_create_quant_cache",
                          QuantConfig(n_layers, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_batch,
                                      max_queries, key_bits, value_bits, _dtype_code(dtype)), dtype, stream)
 
     def _table(self, table, batch):
         """Address and width of the table of a call's sequences."""
-        width = int(table.shape[1]) if getattr(table, "ndim", 0) == 2 else 0
+        shape = getattr(table, "shape", ())
+        width = shape[1] if len(shape) == 2 else 0
         address = self._ints(table, (batch, width), "table")
         if address is None:
             raise TypeError("table must be a CUDA (HIP) tensor")
@@ -51,15 +54,19 @@ class QuantCache(_Handle):
             raise TypeError("%s must be a CUDA (HIP) tensor" % name)
         return address
 
-    def _copy(self, call, layer, k, v, table, start, counts, stream):
-        if getattr(k, "ndim", 0) != 4:
+    def _copy(self, call, name, layer, k, v, table, start, counts, stream):
+        shape = getattr(k, "shape", ())
+        if len(shape) != 4:
             raise TypeError("k must be a CUDA (HIP) tensor [batch][n_kv_heads][tokens][head_dim]")
-        B, tokens = int(k.shape[0]), int(k.shape[2])
+        B, tokens = shape[0], shape[2]
         shape = (B, self.n_kv_heads, tokens, self.head_dim)
         kp, vp = self._tensor(k, shape, "k"), self._tensor(v, shape, "v")
         tp, width = self._table(table, B)
-        _check(getattr(self.lib, call)(self._h, layer, kp, vp, tp, width, self._lengths(start, B, "start"),
-                                       self._ints(counts, (B,), "counts"), B, tokens, _stream(stream, self.device)), call)
+        if stream is None:
+            stream = self._current_stream(self.device)
+        rc = call(self._h, layer, kp, vp, tp, width, self._lengths(start, B, "start"), self._ints(counts, (B,), "counts"), B,
+                  tokens, stream.cuda_stream)
+        _check(rc, name)
 
     def write(self, layer: int, k, v, table, start, counts=None, stream=None):
         """Quantises and stores new tokens (raas_quant_write). k, v:
@@ -67,11 +74,11 @@ class QuantCache(_Handle):
         of each sequence; start: int32 [batch], position of each sequence's first new
         token; counts: int32 [batch], how many of the rows (None: all). All device
         tensors."""
-        self._copy("raas_quant_write", layer, k, v, table, start, counts, stream)
+        self._copy(self._write, "raas_quant_write", layer, k, v, table, start, counts, stream)
 
     def read(self, layer: int, k, v, table, start, counts=None, stream=None):
         """Reads held tokens back into k, v (raas_quant_read); arguments as write."""
-        self._copy("raas_quant_read", layer, k, v, table, start, counts, stream)
+        self._copy(self._read, "raas_quant_read", layer, k, v, table, start, counts, stream)
 
     def attend(self, layer: int, q, out, table, lens, counts=None, lse=None, stream=None):
         """Causal attention of the last tokens' queries over what their sequences hold
