@@ -94,7 +94,8 @@ struct WideBlock {
             }
         }
     };
-    // From a record's address in scalar registers, so that a load's own address costs no vector instruction.
+    // From a record's address in scalar registers (a buffer of its bytes, unstructured), so
+    // that a load's own address costs no vector instruction.
     __device__ __forceinline__ void load(const uint8_t* rec, const Places& at) {
         const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(rec), 0, F::BYTES, 0x00020000);
         auto dwords = [&](uint32_t at, auto& x) {
