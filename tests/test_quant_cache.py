@@ -639,6 +639,22 @@ def test_offsets_past_32_bits():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_tables(dtype):
+    """614588 tokens, most of them the same 512 again and again: a wavefront takes more
+    blocks than its lanes hold pages for at once."""
+    m = Model([700], 4, 1, 64, (4, 8), dtype, page=256, room=300, max_queries=40)
+    p, turns = m.pages[0], 1200
+    m.pages = np.concatenate([np.tile(p[:2], turns), p[2:4]])[None]
+    m.table, m.width = _ints(m.pages), 2 * turns + 2
+    m.K, m.V = ([np.concatenate([np.tile(x[0][:, :512], (1, turns, 1)), x[0][:, 512:]], 1)] for x in (m.K, m.V))
+    m.attend(1)
+    m.attend(40, counts=[3])
+    m.step()
+    m.step()
+
+
+@gpu
 def test_same_bits():
     """The same calls on the same contents."""
     m = Model([7000, 33, 500], 8, 2, 128, (4, 4), page=64, max_queries=5)
