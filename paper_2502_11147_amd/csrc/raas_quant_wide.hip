@@ -33,6 +33,10 @@ constexpr Cut kWideCut = {1024, 8, 8};
 // with bf16 and two products. Probabilities are taken relative to 2^-kRaise of
 // the row's maximum at the time, so they lie below 2^(kRaise + kSlack) and keep all
 // digits down to 2^-14: 2^-21 of the largest or less; below, they are off by 2^-25.
+// That holds for references within kFar of 0, where fp32 has steps of 2^-4: rounding and
+// the lag it causes add one step. From 2^23 on a step is 1, and 2^(kRaise + kSlack + 1) is
+// past fp16's largest number: a wavefront that meets a row beyond kFar starts over with
+// bf16 too.
 template <int VB>
 struct Half {
     static constexpr int kUnit = VB == 4 ? 127 : 120, kLeast = VB == 4 ? 108 : 109, kSpan = VB == 4 ? 32 : 16;
@@ -45,7 +49,7 @@ struct Half {
     static __device__ __forceinline__ uint32_t scaled(uint32_t e) { return e + 0x01010101u * (127 - kUnit); }
     static __device__ __forceinline__ bool outside(u32x2 e) { return (beyond(e[0]) | beyond(e[1])) != 0u; }
 };
-constexpr float kRaise = 7.0f;
+constexpr float kRaise = 7.0f, kFar = 0x1p20f;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -170,7 +174,7 @@ struct Rows {
 };
 
 // Attention of a part into s, from the start. HALF: probabilities and values in fp16;
-// false if a block has an exponent outside.
+// false if a block has an exponent outside, or a row's logits lie far out.
 template <typename T, int D, int KB, int VB, bool HALF>
 __device__ __forceinline__ bool attend_part(const QuantView& L, const QuantAttention& io, const Work& w, const Part& pt,
                                             int lane, Rows<D>& s) {
@@ -183,6 +187,8 @@ __device__ __forceinline__ bool attend_part(const QuantView& L, const QuantAtten
     const typename Wide::Places at(lane);
     int hi = pt.hi;
     bool inside = true;
+    // (looked at after the loop: leaving it where a reference moves took 0.7 % longer)
+    float far = 0.0f;  // how far from 0 the references were
     // channels D/2 h + 8 n .. of the query; an fp32 one's third pieces, for which there is no register left, in LDS
     u32x4 q[D / 16][NQ < 3 ? NQ : 2];
     __shared__ u32x4 third[NQ < 3 ? 1 : D / 16][64];
@@ -251,6 +257,9 @@ __device__ __forceinline__ bool attend_part(const QuantView& L, const QuantAtten
             s.m = m;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s.o[ct] *= alpha;
+            if constexpr (HALF) {
+                far = fmaxf(far, m > kLowest ? fabsf(m) : 0.0f);  // (kLowest: a row that has seen no token)
+            }
         }
         u32x4 p[2][NP];
 #pragma unroll
@@ -300,7 +309,7 @@ __device__ __forceinline__ bool attend_part(const QuantView& L, const QuantAtten
             attend(b + 1, good1, b1);
         }
     }
-    return inside;
+    return inside && __ballot(far > kFar) == 0ull;
 }
 
 template <typename T, int D, int KB, int VB>

@@ -1,0 +1,114 @@
+"""The quantised cache at the ends of what include/raas.h allows: logits far from 0,
+the largest calls, what a handle reserves."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+import quant_reference as ref
+from test_quant_cache import BITS, _dev, _dtype, _ints, _needs_gpu, _np, _within  # noqa: F401  (a fixture)
+
+U32 = ref.U32
+gpu = pytest.mark.gpu
+
+
+def _attend(K, V, q, bits, dtype):
+    """out, lse [queries][hq], [d] of the last queries, as fp64; what the values are held as."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    (hkv, n, d), (queries, hq) = V.shape, q.shape[:2]
+    pages = -(-n // 64)
+    c = raas.QuantCache(1, hq, hkv, d, n_pages=pages, max_batch=1, max_queries=queries, key_bits=bits[0], value_bits=bits[1],
+                        dtype=dtype)
+    table = _ints(np.arange(pages)[None, ::-1])
+    v = _dev(V[None], _dtype(dtype))
+    c.write(0, _dev(K[None], _dtype(dtype)), v, table, _ints([0]))
+    qd = _dev(q[None], _dtype(dtype))
+    assert np.array_equal(_np(qd)[0], q)
+    out, lse = torch.full_like(qd, 9.0), torch.full((1, queries, hq), 9.0, device="cuda")
+    c.attend(0, qd, out, table, _ints([n]), None, lse)
+    c.close()
+    return _np(out)[0], _np(lse)[0], ref.held(_np(v)[0], bits[1])
+
+
+def _check(got, gl, V, gaps, x, largest, dtype, half, what):
+    """gaps [n]: what token j's logit, all of whose sums are exact, lies above x [queries][hq]. Softmax
+    does not depend on x: the exponent fma(logit, scale, -m) is a difference of two
+    neighbours, rounded once at its own size, and a reference m that is rounded at the
+    logits' size moves all probabilities of a row by one factor. So a probability is off
+    by (n + 64 + 4 max gap) u of itself, an output as tests/quant_reference.py says
+    beyond that; a log-sum-exp moves by a few roundings at its size."""
+    queries, hq, d = got.shape
+    hkv, n = V.shape[:2]
+    for i in range(queries):
+        last = n - queries + i + 1
+        e = np.exp(gaps[:last] - gaps[:last].max())
+        a = e / e.sum()
+        rel = (last + 64 + 4 * np.ptp(gaps[:last]) + (0 if dtype == "bf16" else 2 * last)) * U32
+        log = x[i] + gaps[:last].max() + math.log(e.sum())
+        assert (np.abs(gl[i] - log) <= 8 * U32 * np.abs(largest) + rel).all(), (what, i, gl[i], log)
+        for h in range(hkv):
+            want, A = a @ V[h, :last], a @ np.abs(V[h, :last])
+            bound = rel * A
+            if dtype == "bf16":
+                bound = bound + (2.0 ** -11 * A + 2.0 ** -32 * a.max() * np.abs(V[h, :last]).sum(0) if half else 2.0 ** -15 * A)
+                bound = bound + 2.0 ** -8 * (np.abs(want) + bound)
+            heads = slice(h * hq // hkv, (h + 1) * hq // hkv)
+            _within(got[i, heads], np.broadcast_to(want, got[i, heads].shape), np.broadcast_to(bound, got[i, heads].shape),
+                    what + (i, h))
+
+
+def _queries(rng, x, d, queries, hq):
+    """Constants, one a row, that keys of 6144 turn into logits up to x; their logits."""
+    c = x * rng.uniform(0.9, 1.0, (queries, hq, 1)) / (6144.0 * math.sqrt(d))
+    unit = 2.0 ** np.floor(np.log2(c) - 7)
+    c = np.floor(c / unit) * unit  # bf16
+    return c, (c * 6144.0 * d / math.sqrt(d))[..., 0]
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("queries", [1, 6, 40])
+def test_equal_logits_far_out(queries, dtype, bits, d):
+    """All tokens' logits equal, up to +-4.99e8: even weights, the values' mean, also of large values."""
+    rng = np.random.default_rng(queries + d + bits[0])
+    hkv, n = 2, 300
+    hq = 4
+    for x in (1e5, 3e6, 2e7, 6e7, 1.2e8, 2.08e8, 3e8, 4.2e8, 4.99e8):
+        for sign in (1.0, -1.0):
+            for size in (1.0, 2.0 ** 70):
+                c, logit = _queries(rng, x, d, queries, hq)
+                V = rng.standard_normal((hkv, n, d)) * size
+                got, gl, held = _attend(np.full((hkv, n, d), sign * 6144.0), V, np.broadcast_to(c, (queries, hq, d)), bits, dtype)
+                _check(got, gl, held, np.zeros(n), sign * logit, x, dtype, queries * hq // hkv > 16, (x, sign, size))
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("queries", [1, 40])
+def test_rising_logits_far_out(queries, dtype, bits, d):
+    """Logits that rise from block to block by a few units (a channel of small queries:
+    every sum is a multiple of 32 below 2^29, thus exact), while all lie far from 0."""
+    rng = np.random.default_rng(queries + d + bits[1])
+    hkv, hq, n = 2, 4, 300
+    steps = np.array([0, 1, 2, 3, 4, 6, 8, 12])  # times 512: the 4-bit grid beside 6144
+    at = steps[np.minimum(np.arange(n) // 32, 7)]
+    for x in (1e5, 2e6, 1e7, 2.5e7, 4e7):
+        for sign in (1.0, -1.0):
+            c, _ = _queries(rng, x, d, queries, hq)
+            q = np.repeat(c, d, axis=2)
+            q[..., 0] = 2.0 ** -4
+            K = np.full((hkv, n, d), sign * 6144.0)
+            K[..., 0] = 512.0 * at
+            V = rng.standard_normal((hkv, n, d))
+            got, gl, held = _attend(K, V, q, bits, dtype)
+            logit = sign * (c * 6144.0 * (d - 1) / math.sqrt(d))[..., 0]
+            _check(got, gl, held, 32.0 * at / math.sqrt(d), logit, x, dtype, queries * hq // hkv > 16, (x, sign))
