@@ -449,10 +449,10 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
  *
  * The conventions at the top hold: device tensors (aligned to their element type),
  * nothing awaited (but by the destroy), finite inputs (scaled logits within 5e8 of
- * 0, as above, values within 2^100), calls on one handle, and graphs of them, ordered (attention and
- * steps share its scratch). Nothing is allocated after the creation. The same calls
- * on the same contents give the same bits. A handle's calls run on the device that
- * was current at its creation. */
+ * 0, as above, values within 2^75 where attention reads them), calls on one handle,
+ * and graphs of them, ordered (attention and steps share its scratch). Nothing is
+ * allocated after the creation. The same calls on the same contents give the same
+ * bits. A handle's calls run on the device that was current at its creation. */
 typedef struct {
     int32_t n_layers;    /* >= 1 */
     int32_t n_q_heads;   /* multiple of n_kv_heads, group G = n_q_heads/n_kv_heads <= 16 */

@@ -76,13 +76,14 @@ def _queries(rng, x, d, queries, hq):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("queries", [1, 6, 40])
 def test_equal_logits_far_out(queries, dtype, bits, d):
-    """All tokens' logits equal, up to +-4.99e8: even weights, the values' mean, also of large values."""
+    """All tokens' logits equal, up to +-4.99e8: even weights, the values' mean, up to values of
+    2^75 (2^72 times normal numbers) and far below 1."""
     rng = np.random.default_rng(queries + d + bits[0])
     hkv, n = 2, 300
     hq = 4
     for x in (1e5, 3e6, 2e7, 6e7, 1.2e8, 2.08e8, 3e8, 4.2e8, 4.99e8):
         for sign in (1.0, -1.0):
-            for size in (1.0, 2.0 ** 70):
+            for size in (1.0, 2.0 ** 72, 2.0 ** -60):
                 c, logit = _queries(rng, x, d, queries, hq)
                 V = rng.standard_normal((hkv, n, d)) * size
                 got, gl, held = _attend(np.full((hkv, n, d), sign * 6144.0), V, np.broadcast_to(c, (queries, hq, d)), bits, dtype)
