@@ -1,5 +1,5 @@
 """The kernels of the quantised cache's steps and of attention of few rows: both kinds of
-loads, wavefronts of 0 to 10 and of more than 64 blocks."""
+loads, wavefronts of 0 to 10 and of more than 64 blocks, parts joined with a prefix's."""
 from __future__ import annotations
 
 import ctypes
@@ -191,3 +191,26 @@ def test_more_turns_than_lanes(dtype, bits, d):
     x = Held(lens, 4, 1, d, bits, dtype, 256, 8, seed=d + bits[1], missing=20)
     x.check(0, [0, 3, 40])
     x.check(4, [1, 65])
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(4, 1, 64), (16, 1, 128), (14, 2, 64), (6, 2, 128)], ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parts_joined_with_a_prefix(dtype, shape):
+    """Steps of sequences in 64, 12 and 1 parts beside a prefix in many or one: more sources than lanes."""
+    import paper_2502_11147_amd as raas
+
+    hq, hkv, d = shape
+    lens = [20000, 601, 5, 0, 2900]
+    x = Held(lens, hq, hkv, d, BITS[hq % 4], dtype, 64, 40, seed=hq)
+    plan = x.cache.lib._ZN4raas11plan_prefixEiiib
+    plan.restype, plan.argtypes = ctypes.c_int, [ctypes.c_int] * 3 + [ctypes.c_bool]
+    parts = _cut([-(-(n + 1) // BLOCK) for n in lens], hkv)
+    sources = []
+    for tokens in (4000, 300, 1, 0):
+        p = raas.SharedPrefix(1, hq, hkv, d, 4000, len(lens), dtype)
+        (k, kn), (v, vn) = x.data(hkv, max(tokens, 1), d), x.data(hkv, max(tokens, 1), d)
+        p.store(0, k if tokens else None, v if tokens else None)
+        sources.append(parts[0][0] + plan(hkv, len(lens) * hq // hkv, tokens, dtype == "bf16"))
+        x.check(0, range(len(lens)), (p, kn[:, :tokens], vn[:, :tokens]))
+    assert parts[0][0] == 64 and parts[1][0] == 1 and parts[4][0] == 12 and max(sources) > 64, (parts, sources)
