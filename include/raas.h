@@ -505,8 +505,10 @@ raas_status raas_quant_read(raas_quant_cache* cache, int32_t layer, void* k, voi
  * entry above `queries`: queries; lens past the table's row count as its end. out
  * like q, and, unless NULL, lse [batch][queries][n_q_heads] (fp32): the natural
  * logarithm of the sum of the exponentials of the scaled logits. A query that sees
- * no token has out 0 and lse -inf. Rows from counts[b] on, and those of sequences
- * of negative length, stay as they are. Errors: RAAS_E_INVALID, RAAS_E_HIP. */
+ * no token has out 0 and lse -inf. A NaN group of a held value
+ * reaches the channels of that group, one of a key all channels and lse, of the
+ * queries that see the token, and of no other. Rows from counts[b] on, and those of
+ * sequences of negative length, stay as they are. Errors: RAAS_E_INVALID, RAAS_E_HIP. */
 raas_status raas_quant_attention(raas_quant_cache* cache, int32_t layer, const void* q, const int32_t* table,
                                  int32_t table_width, const int32_t* lens, const int32_t* counts, int32_t batch,
                                  int32_t queries, void* out, float* lse, void* stream);

@@ -267,6 +267,29 @@ __device__ __forceinline__ void follow(const f32x4 (&x)[RT][2], float scale_log2
     }
 }
 
+// A block some of whose tokens not every row sees, with NaN among its values: a product
+// would give it to all rows, a masked probability being 0. The NaN go to the outputs of
+// the rows that see them (tokens below lim) and become numbers in the block.
+template <int D, int KB, int VB>
+__device__ __forceinline__ void hand_out_nan(Block<D, KB, VB>& blk, int lim, int a, Softmax<D>& s) {
+    using F = Format<D, KB, VB>;
+    const uint32_t own = nan_mask(blk.ve);
+    // tokens with NaN in this lane's outputs, channels D/4 a .., which lie in one group
+    uint32_t all = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) all |= (uint32_t)__shfl((int)own, 16 * b + F::kgroup(a) * F::VSHARE) << (8 * b);
+    const bool hit = lim > 0 && (all << (32 - min(lim, 32))) != 0u;
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct)
+        if (hit) s.o[ct] = f32x4{NAN, NAN, NAN, NAN};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (own >> j & 1u) {
+            if constexpr (VB == 8) blk.set_value(j, u32x2{0u, 0u});  // (4 bits have no NaN of their own)
+            blk.set_exponent(j, 120u);
+        }
+}
+
 // One block against RT tiles of 16 rows.
 template <typename T, int D, int KB, int VB, int RT>
 __device__ __forceinline__ void attend_block(const Block<D, KB, VB>& blk, const u32x4 (&q)[RT][D / 32][kQueryPieces<T>],

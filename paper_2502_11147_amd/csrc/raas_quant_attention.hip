@@ -148,6 +148,10 @@ template <typename T, int KB, int VB, bool STREAM>
 constexpr int kStreamBlocks = STREAM && KB + VB == 8 && sizeof(T) == 2 ? 4 : 2;
 template <typename T, int KB, int VB, bool STREAM>
 constexpr int kStreamPerSimd = sizeof(T) == 4 ? 1 : kStreamBlocks<T, KB, VB, STREAM> == 4 ? 2 : 3;
+// Not more than two either: with three, for which its registers would do, it takes 200 us.
+// (head_dim 64: 200 with four, 226 with two.)
+template <typename T, int D, int KB, int VB, bool STREAM>
+constexpr int kStreamMost = kStreamBlocks<T, KB, VB, STREAM> == 4 && D == 128 ? 2 : 8;
 // Parts: of 8 KV heads with 30000 tokens in 64, 43 and 32 parts 17.9, 17.0 and 15.2 us:
 // publishing a part and joining it costs more than a workgroup's share of an even
 // load, once every compute unit has one. One sequence of 1000 tokens takes 8.2, 8.8
@@ -159,8 +163,8 @@ constexpr Cut kStreamCut = {256, 4, 20};
 
 template <typename T, int D, int KB, int VB, bool STREAM>
 __global__ __launch_bounds__(kStreamWaves * 64)
-__attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_quant_stream(QuantView L,
-                                                                                            QuantAttention io) {
+__attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>, kStreamMost<T, D, KB, VB, STREAM>)))
+void k_quant_stream(QuantView L, QuantAttention io) {
     using F = Format<D, KB, VB>;
     constexpr int NW = kStreamWaves, NB = kStreamBlocks<T, KB, VB, STREAM>;
     __shared__ __align__(16) float s_o[NW][16][D + 4];
@@ -202,10 +206,12 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_q
         page[I] = page[I] >= 0 && page[I] < L.n_pages ? page[I] : -1;
         ring[I].template load<STREAM>(record<F>(L, max(page[I], 0), lo + wv + turn * NW, w.h), lane);
     };
-    auto attend = [&](int b, Block<D, KB, VB>& blk) {
-        const int t0 = b * kQuantBlock;
-        const int l[1] = {lim - t0};
-        attend_block<T, D, KB, VB, 1>(blk, q, t0 + kQuantBlock > least, l, a, io.scale_log2, s);
+    // A row's limit lies within 16 tokens of the end, that is in the last two blocks, which
+    // different wavefronts take, each as its last.
+    static_assert(kStreamRows <= kQuantBlock && NW >= 2, "");
+    auto attend = [&](int b, Block<D, KB, VB>& blk, bool masked) {
+        const int l[1] = {lim - b * kQuantBlock};
+        attend_block<T, D, KB, VB, 1>(blk, q, masked, l, a, io.scale_log2, s);
     };
     if (turns > 0) {
         fetch(0, Int<0>());
@@ -223,7 +229,7 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_q
                 return false;
             }
             fetch(turn + NB - 1, Int<LAST>());
-            if (page[I] >= 0) attend(lo + wv + turn * NW, ring[I]);
+            if (page[I] >= 0) attend(lo + wv + turn * NW, ring[I], false);
             ++turn;
             return true;
         };
@@ -241,7 +247,9 @@ __attribute__((amdgpu_waves_per_eu(kStreamPerSimd<T, KB, VB, STREAM>))) void k_q
                 take_token<T, D, KB, VB>(io, blk, record<F>(L, page[0], b, w.h), w.fresh - t0, (size_t)w.b * L.nkv + w.h,
                                          lane);
             if (t0 + kQuantBlock > w.tokens) blk.zero_values_from(w.tokens - t0, a);
-            attend(b, blk);
+            const bool masked = t0 + kQuantBlock > least;
+            if (masked && __ballot(any_nan(blk.ve)) != 0ull) hand_out_nan<D, KB, VB>(blk, lim - t0, a, s[0]);
+            attend(b, blk, masked);
         }
     }
     const float sum = sum_groups(s[0].l);

@@ -71,6 +71,14 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t four, int j) {
     return j == 0 ? four << 23 : j == 1 ? four << 15 : j == 2 ? four << 7 : four >> 1;
 }
 
+// The bytes of 255 among four exponents, NaN: their uppermost bits; of eight: bit j of byte j.
+__device__ __forceinline__ uint32_t nan_bits(uint32_t e) { return ((e & 0x7F7F7F7Fu) + 0x01010101u) & e & 0x80808080u; }
+__device__ __forceinline__ bool any_nan(u32x2 e) { return (nan_bits(e[0]) | nan_bits(e[1])) != 0u; }
+__device__ __forceinline__ uint32_t nan_mask(u32x2 e) {
+    // (bits 0, 8, 16, 24 to 24 .. 27; the other products meet neither these nor each other)
+    return ((nan_bits(e[0]) >> 7) * 0x01020408u >> 24 & 15u) | ((nan_bits(e[1]) >> 7) * 0x01020408u >> 20 & 240u);
+}
+
 // Two codes, from byte `at` of a dword (a constant once loops are unrolled), as bf16 or (HALF) fp16.
 template <int BITS, bool HALF>
 __device__ __forceinline__ uint32_t two_values(uint32_t x, int at, float scale) {

@@ -127,17 +127,40 @@ struct WideBlock {
             ve[x] = __builtin_amdgcn_raw_buffer_load_b64(from, at.ve[x], 0, 0);
         }
     }
-    // Values of tokens `valid` .. of the block become 0, whatever is stored there.
-    __device__ __forceinline__ void zero_values_from(int valid, int h) {
+    // Token 16 x + 8 h + j's value becomes 0.
+    __device__ __forceinline__ void clear(int x, int j) {
         constexpr int PER = 4 / F::VHALF;  // tokens of a dword
+        v[x][j / PER] &= PER == 1 ? 0u : ~((0xFFFFFFFFu >> (32 - 32 / PER)) << (32 / PER * (j % PER)));
+        ve[x][j >> 2] = (ve[x][j >> 2] & ~(255u << (8 * (j & 3)))) | 120u << (8 * (j & 3));
+    }
+    // Those of tokens `valid` .. of the block, whatever is stored there.
+    __device__ __forceinline__ void zero_values_from(int valid, int h) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (16 * x + 8 * h + j >= valid) {
-                    v[x][j / PER] &= PER == 1 ? 0u : ~((0xFFFFFFFFu >> (32 - 32 / PER)) << (32 / PER * (j % PER)));
-                    ve[x][j >> 2] = (ve[x][j >> 2] & ~(255u << (8 * (j & 3)))) | 120u << (8 * (j & 3));
-                }
+                if (16 * x + 8 * h + j >= valid) clear(x, j);
+    }
+    // As hand_out_nan: a lane's outputs o are those of one row and of 8 consecutive
+    // places of r for each group of channels (head_dim 128: of 4).
+    __device__ __forceinline__ void hand_out_nan(int lim, f32x16 (&o)[D / 32]) {
+        constexpr int EACH = 32 / F::NG;  // lanes i of a group; half as many r
+        const uint32_t own = nan_mask(ve[0]) | nan_mask(ve[1]) << 8;  // tokens 8 h .., 16 + 8 h ..
+#pragma unroll
+        for (int g = 0; g < F::NG; ++g) {
+            const uint32_t x = __builtin_amdgcn_readlane(own, EACH * g), y = __builtin_amdgcn_readlane(own, 32 + EACH * g);
+            const uint32_t all = (x & 255u) | (y & 255u) << 8 | (x & 0xFF00u) << 8 | (y & 0xFF00u) << 16;
+            const bool hit = lim > 0 && (all << (32 - min(lim, 32))) != 0u;
+#pragma unroll
+            for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+                for (int r = EACH / 2 * g; r < EACH / 2 * (g + 1); ++r) o[ct][r] = hit ? NAN : o[ct][r];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (own >> (8 * x + j) & 1u) clear(x, j);
     }
     // Channels 8 n .. + 7 of this lane's key, as bf16.
     __device__ __forceinline__ u32x4 key(int n) const {
@@ -234,6 +257,9 @@ __device__ __forceinline__ bool attend_part(const QuantView& L, const QuantAtten
             }
         }
         if (!good) return;
+        if constexpr (!HALF) {  // (fp16: NaN are outside)
+            if (masked && __ballot(any_nan(blk.ve[0]) || any_nan(blk.ve[1])) != 0ull) blk.hand_out_nan(lim - t0, s.o);
+        }
         f32x16 x = zero;
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) {
