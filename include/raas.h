@@ -460,7 +460,7 @@ typedef struct {
     int32_t head_dim;    /* 64 or 128 */
     int32_t page_size;   /* tokens per page: 32, 64, 128 or 256 */
     int32_t n_pages;     /* pages of a layer, >= 1 */
-    int32_t max_batch;   /* sequences per call, 1 .. 4096 */
+    int32_t max_batch;   /* sequences per call, 1 .. 4096; max_batch * n_kv_heads <= 8388608 */
     int32_t max_queries; /* queries per sequence of raas_quant_attention, >= 1;
                             max_batch * max_queries * n_q_heads <= 16777216 */
     int32_t key_bits;    /* 4 or 8 */

@@ -12,9 +12,10 @@ using namespace raas;
 
 namespace {
 
-// Sequences and queries per sequence of one call, and rows of a call's heads
-// (the grids' limits; every workgroup reads all lengths).
-constexpr int kMaxBatch = 4096, kMaxCallRows = 1 << 24;
+// Sequences of a call (every workgroup reads all lengths), KV heads of them all (a
+// workgroup of 256 threads each and those of cut ones: a launch has below 2^32 threads;
+// 2^15 blocks of each, a 256th of them to a workgroup, are below 2^31), rows of their heads.
+constexpr int kMaxBatch = 4096, kMaxUnits = 1 << 23, kMaxCallRows = 1 << 24;
 
 }  // namespace
 
@@ -121,6 +122,9 @@ raas_status raas_create_quant_cache(const raas_quant_config* cfg, void* stream, 
     if (cfg->n_pages < 1) return fail(RAAS_E_INVALID, "n_pages must be >= 1 (got %d)", cfg->n_pages);
     if (cfg->max_batch < 1 || cfg->max_batch > kMaxBatch)
         return fail(RAAS_E_INVALID, "max_batch must lie in [1, %d] (got %d)", kMaxBatch, cfg->max_batch);
+    if ((double)cfg->max_batch * cfg->n_kv_heads > kMaxUnits)
+        return fail(RAAS_E_INVALID, "max_batch * n_kv_heads must be at most %d (got %d * %d)", kMaxUnits, cfg->max_batch,
+                    cfg->n_kv_heads);
     if (cfg->max_queries < 1 || (double)cfg->max_batch * cfg->max_queries * cfg->n_q_heads > kMaxCallRows)
         return fail(RAAS_E_INVALID, "max_queries must be >= 1, and max_batch * max_queries * n_q_heads at most %d (got %d)",
                     kMaxCallRows, cfg->max_queries);

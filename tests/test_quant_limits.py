@@ -2,13 +2,14 @@
 the largest calls, what a handle reserves."""
 from __future__ import annotations
 
+import ctypes
 import math
 
 import numpy as np
 import pytest
 
 import quant_reference as ref
-from test_quant_cache import BITS, _dev, _dtype, _ints, _needs_gpu, _np, _within  # noqa: F401  (a fixture)
+from test_quant_cache import BITS, _config, _dev, _dtype, _ints, _needs_gpu, _np, _within, lib  # noqa: F401  (fixtures)
 
 U32 = ref.U32
 gpu = pytest.mark.gpu
@@ -113,3 +114,48 @@ def test_rising_logits_far_out(queries, dtype, bits, d):
             got, gl, held = _attend(K, V, q, bits, dtype)
             logit = sign * (c * 6144.0 * (d - 1) / math.sqrt(d))[..., 0]
             _check(got, gl, held, 32.0 * at / math.sqrt(d), logit, x, dtype, queries * hq // hkv > 16, (x, sign))
+
+
+@pytest.mark.parametrize("units,refused", [(4096 * 2048, False), (4096 * 2049, True), (4096 * 4096, True)])
+def test_units_of_a_call(lib, units, refused):  # noqa: F811
+    """max_batch * n_kv_heads workgroups and those of cut sequences, of 256 threads, are within 2^32."""
+    import paper_2502_11147_amd as raas
+
+    heads = units // 4096
+    cfg = _config(n_layers=1, n_q_heads=heads, n_kv_heads=heads, head_dim=64, page_size=32, n_pages=1, max_batch=4096,
+                  max_queries=1)
+    h = ctypes.c_void_p()
+    code = lib.raas_create_quant_cache(ctypes.byref(cfg), None, ctypes.byref(h))
+    assert (code == raas.E_INVALID) == refused  # (without a GPU a call in range fails otherwise)
+    if refused:
+        assert b"max_batch * n_kv_heads" in lib.raas_last_error()
+    lib.raas_destroy_quant_cache(h)
+
+
+@gpu
+def test_the_most_units():
+    """4096 sequences of 2048 KV heads, all behind one page."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    B, H, d, n = 4096, 2048, 64, 31
+    rng = np.random.default_rng(1)
+    c = raas.QuantCache(1, H, H, d, n_pages=1, page_size=32, max_batch=B)
+    k, v = (_dev(rng.standard_normal((1, H, n, d)).astype(np.float32), torch.bfloat16) for _ in range(2))
+    c.write(0, k, v, _ints([[0]]), _ints([0]))
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.randn(B, 1, H, d, generator=g, device="cuda", dtype=torch.bfloat16)
+    out, lse = torch.full_like(q, 9.0), torch.full((B, 1, H), 9.0, device="cuda")
+    c.attend(0, q, out, torch.zeros(B, 1, dtype=torch.int32, device="cuda"), _ints([n] * B), None, lse)
+    K, V = ref.held(_np(k)[0], 4), ref.held(_np(v)[0], 4)
+    b = np.concatenate([[0, B - 1, 0, B - 1], rng.integers(0, B, 300)])
+    h = np.concatenate([[0, H - 1, H - 1, 0], rng.integers(0, H, 300)])
+    at = torch.from_numpy(b).cuda(), 0, torch.from_numpy(h).cuda()
+    got, gl, qn = _np(out[at]), _np(lse[at]), _np(q[at])
+    for i in range(len(b)):
+        o, ob, l, lb = ref.attention(qn[i][None], K[h[i]], V[h[i]], True)
+        _within(got[i][None], o, ob, ("out", b[i], h[i]))
+        _within(gl[i][None], l, lb, ("lse", b[i], h[i]))
+    assert not (lse == 9.0).any()
+    c.close()
