@@ -318,7 +318,8 @@ QuantScratch quant_scratch(int batch, int queries, int nkv, int G) {
     // (A unit's rows are one tile here.)
     const size_t units = (size_t)batch * nkv;
     const size_t rows = std::min((size_t)2 * kStreamCut.target, units * kMaxQuantParts) * kStreamRows;
-    return {std::max(rows, quant_wide_scratch_rows(batch, queries, nkv, G)), units};
+    const size_t wide = queries * G > kStreamRows ? quant_wide_scratch_rows(batch, queries, nkv, G) : 0;
+    return {std::max(rows, wide), units};
 }
 
 hipError_t launch_quant_attention(const QuantView& L, bool bf16, const QuantAttention& io, bool stream, hipStream_t s) {

@@ -159,3 +159,23 @@ def test_the_most_units():
         _within(gl[i][None], l, lb, ("lse", b[i], h[i]))
     assert not (lse == 9.0).any()
     c.close()
+
+
+class _Scratch(ctypes.Structure):  # raas::QuantScratch
+    _fields_ = [("rows", ctypes.c_size_t), ("arrivals", ctypes.c_size_t)]
+
+
+def _scratch(lib, batch, queries, hkv, G):  # noqa: F811
+    f = lib._ZN4raas13quant_scratchEiiii
+    f.restype, f.argtypes = _Scratch, [ctypes.c_int] * 4
+    x = f(batch, queries, hkv, G)
+    return x.rows, x.arrivals
+
+
+def test_scratch_is_that_of_the_calls_that_can_be(lib):  # noqa: F811
+    """Rows of parts: 2 * 256 slots of 16 rows for up to 16 rows per KV head, 2 * 1024 of 32 beyond,
+    64 per tile if that is less."""
+    for batch, queries, hkv, G, rows in ((128, 1, 8, 4, 512 * 16), (128, 4, 8, 4, 512 * 16), (1, 16, 2, 1, 128 * 16),
+                                         (128, 5, 8, 4, 2048 * 32), (1, 17, 2, 1, 128 * 32), (1, 40, 2, 1, 256 * 32),
+                                         (4096, 1, 2048, 1, 512 * 16)):
+        assert _scratch(lib, batch, queries, hkv, G) == (rows, batch * hkv)
