@@ -443,8 +443,8 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
  * layer has pages of its own under the same numbers. A page may stand in a table
  * more than once (sequences that share a prompt) if the call writes none of its
  * tokens. Tokens whose entry is no page, or that lie past the table's
- * row, are neither written, read nor attended to. Tokens that were never written
- * hold anything. Table, lengths and counts are read when the call runs, so that
+ * row, are neither written, read nor attended to. Tokens that were never written are
+ * zeros. Table, lengths and counts are read when the call runs, so that
  * calls may be captured into a HIP graph: a replay works on what they hold then.
  *
  * The conventions at the top hold: device tensors (aligned to their element type),

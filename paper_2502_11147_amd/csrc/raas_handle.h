@@ -87,9 +87,9 @@ struct Req {
 };
 
 // One allocation, cut into parts of 256 bytes and up (an allocation takes some
-// 30 us); what must start at zero is cleared on the stream. Keys, values and
-// scratch need not: no place is looked at before it is written, but for the rest
-// of a block, whose logits and values are masked.
+// 30 us); what must start at zero is cleared on the stream. Scratch, and keys and
+// values of a weight cache or a prefix, need not: no place is looked at before it is
+// written, but for the rest of a block, whose logits and values are masked.
 inline raas_status allocate(const std::vector<Req>& reqs, void** base, size_t& total, hipStream_t s) {
     auto padded = [](size_t n) { return (n + 255) & ~(size_t)255; };
     total = 0;

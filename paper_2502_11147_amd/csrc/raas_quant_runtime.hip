@@ -155,7 +155,7 @@ raas_status raas_create_quant_cache(const raas_quant_config* cfg, void* stream, 
             {(void**)&c->arrived, x.arrivals * 4, true},
             {(void**)&c->part, x.rows * cfg->head_dim * 4, false},
             {(void**)&c->ml, x.rows * 2 * 4, false},
-            {&c->pool, c->layer_bytes * cfg->n_layers, false},
+            {&c->pool, c->layer_bytes * cfg->n_layers, true},  // (a table may name tokens that no call has written)
         };
         const raas_status sa = allocate(reqs, &c->memory, c->bytes, (hipStream_t)stream);
         if (sa != RAAS_OK) {

@@ -179,3 +179,36 @@ def test_scratch_is_that_of_the_calls_that_can_be(lib):  # noqa: F811
                                          (128, 5, 8, 4, 2048 * 32), (1, 17, 2, 1, 128 * 32), (1, 40, 2, 1, 256 * 32),
                                          (4096, 1, 2048, 1, 512 * 16)):
         assert _scratch(lib, batch, queries, hkv, G) == (rows, batch * hkv)
+
+
+@gpu
+@pytest.mark.parametrize("queries", [1, 20])
+@pytest.mark.parametrize("pages", [40, 9000])
+def test_tokens_never_written(pages, queries):
+    """A new cache's tokens are zeros, also where another's lay before: NaN in every page of it."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    make = lambda: raas.QuantCache(2, 4, 2, 128, n_pages=pages, page_size=256, max_batch=1, max_queries=20,  # noqa: E731
+                                   key_bits=8, value_bits=4)
+    n = min(pages, 4096) * 256
+    nan = torch.full((1, 2, n, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(pages - n // 256, pages, dtype=torch.int32, device="cuda")[None]
+    c = make()
+    for layer in range(2):
+        c.write(layer, nan, nan, table, _ints([0]))
+    torch.cuda.synchronize()
+    c.close()
+    c = make()
+    out = torch.full((1, queries, 4, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((1, queries, 4), 9.0, device="cuda")
+    for layer in range(2):
+        k, v = torch.full_like(nan, 9.0), torch.full_like(nan, 9.0)
+        c.read(layer, k, v, table, _ints([0]))
+        assert not k.any() and not v.any()
+        c.attend(layer, torch.randn_like(out), out, table, _ints([n]), None, lse)
+        assert not out.any()
+        want = np.log(n - queries + 1.0 + np.arange(queries))
+        assert np.abs(_np(lse)[0] - want[:, None]).max() <= (n + 64) * U32 + 8 * U32 * want.max()
+    c.close()
