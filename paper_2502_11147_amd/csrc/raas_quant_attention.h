@@ -286,7 +286,7 @@ __device__ __forceinline__ void hand_out_nan(Block<D, KB, VB>& blk, int lim, int
     for (int j = 0; j < 8; ++j)
         if (own >> j & 1u) {
             if constexpr (VB == 8) blk.set_value(j, u32x2{0u, 0u});  // (4 bits have no NaN of their own)
-            blk.set_exponent(j, 120u);
+            blk.set_exponent(j, kZeroExponent);
         }
 }
 

@@ -10,8 +10,8 @@
 // 2^23 minus the mantissa of 1.75 (1.8125) moves into the next binade exactly the
 // maxima that reach it. Products with powers of two are exact, so codes do not
 // depend on how they are computed. e lies in 16 .. 252 (246): below, codes times X
-// would leave the normal range of bf16, above, its largest. A group that holds
-// an infinity or NaN has e = 255 and reads as NaN.
+// would leave the normal range of bf16, above, its largest. A group of zeros has
+// e = 120, one that holds an infinity or NaN e = 255, which reads as NaN.
 //
 // Layout: codes lie in the order in which the lanes of v_mfma_f32_16x16x32_bf16
 // take their operands once they are converted, so a wavefront reads 1 KiB of
@@ -63,6 +63,9 @@ struct Format {
     static __device__ __forceinline__ int vgroup(int i) { return i * VC / kQuantGroup; }
     static constexpr int VSHARE = kQuantGroup / VC;
 };
+
+// Exponent byte of a group of zeros.
+constexpr uint32_t kZeroExponent = 120;
 
 // The scale operand of a conversion, whose exponent alone counts (its sign and
 // mantissa may be anything): of an exponent byte, and of byte j of four.
@@ -155,7 +158,7 @@ struct Values {
         for (int j = 0; j < 8; ++j)
             if (8 * a + j >= valid) {
                 set_value(j, u32x2{0u, 0u});
-                set_exponent(j, 120u);
+                set_exponent(j, kZeroExponent);
             }
     }
     __device__ __forceinline__ void set_exponent(int j, uint32_t e) {
@@ -224,13 +227,14 @@ struct Block : Keys<D, KB, VB>, Values<D, KB, VB> {
     }
 };
 
-// Exponent byte of a group whose largest magnitude is `most`.
+// Exponent byte of a group whose largest magnitude is `most`. (One of zeros may have any: that
+// of numbers near 1 keeps their tokens with the others in the kernel for many rows.)
 template <int BITS>
 __device__ __forceinline__ uint32_t exponent_of(float most) {
     const uint32_t b = __float_as_uint(most);
     if (b >= 0x7F800000u) return 255u;
     const int e = (int)((b + (BITS == 4 ? 0x200000u : 0x180000u)) >> 23) - (BITS == 4 ? 2 : 8);
-    return (uint32_t)min(max(e, 16), BITS == 4 ? 252 : 246);
+    return (uint32_t)min(max(e, b == 0u ? (int)kZeroExponent : 16), BITS == 4 ? 252 : 246);
 }
 
 // N (a multiple of 4) values to N * BITS / 8 bytes of codes, in dwords (the upper

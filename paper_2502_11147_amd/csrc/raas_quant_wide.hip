@@ -49,6 +49,8 @@ struct Half {
     static __device__ __forceinline__ uint32_t scaled(uint32_t e) { return e + 0x01010101u * (127 - kUnit); }
     static __device__ __forceinline__ bool outside(u32x2 e) { return (beyond(e[0]) | beyond(e[1])) != 0u; }
 };
+static_assert(kZeroExponent >= Half<8>::kLeast && kZeroExponent < Half<8>::kLeast + Half<8>::kSpan &&
+                  kZeroExponent >= Half<4>::kLeast && kZeroExponent < Half<4>::kLeast + Half<4>::kSpan, "");
 constexpr float kRaise = 7.0f, kFar = 0x1p20f;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -131,7 +133,7 @@ struct WideBlock {
     __device__ __forceinline__ void clear(int x, int j) {
         constexpr int PER = 4 / F::VHALF;  // tokens of a dword
         v[x][j / PER] &= PER == 1 ? 0u : ~((0xFFFFFFFFu >> (32 - 32 / PER)) << (32 / PER * (j % PER)));
-        ve[x][j >> 2] = (ve[x][j >> 2] & ~(255u << (8 * (j & 3)))) | 120u << (8 * (j & 3));
+        ve[x][j >> 2] = (ve[x][j >> 2] & ~(255u << (8 * (j & 3)))) | kZeroExponent << (8 * (j & 3));
     }
     // Those of tokens `valid` .. of the block, whatever is stored there.
     __device__ __forceinline__ void zero_values_from(int valid, int h) {

@@ -57,3 +57,27 @@ def test_nan_of_later_tokens(hq, queries, dtype, bits, d):
                 o, ob, l, lb = ref.attention(qn[b, i, heads], K[b, h, :last], V[b, h, :last], m.bf16, half=queries * G > 16)
                 _within(gl[b, i, heads], l, lb, ("lse",) + what)
                 _within(got[b, i, heads][:, ~nan], o[:, ~nan], ob[:, ~nan], ("out",) + what)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bits", BITS, ids=str)
+def test_groups_of_zeros(bits, d):
+    """Padded or silent tokens read as zeros and leave the other channels' outputs the same bits."""
+    import torch
+
+    n, queries = 700, 40
+    outs, V = [], None
+    for zeros in (False, True):
+        m = Model([0, 0], 4, 2, d, bits, page=64, width=11, max_queries=queries, seed=9)
+        (k, kn), (v, vn) = m.data(2, 2, n, d), m.data(2, 2, n, d)
+        if zeros:
+            v[0, :, 0, :32], v[0, 1, 650, :32], v[1, :, 300:, :32] = 0, -0.0, 0
+            vn = _np(v)
+        m.cache.write(0, k, v, m.table, _ints([0, 0]))
+        for b in range(2):
+            m.K[b], m.V[b] = ref.held(kn[b], bits[0]), ref.held(vn[b], bits[1])
+        m.check_held()
+        outs.append(m.attend(queries))
+    (a, la), (b, lb) = outs
+    assert torch.equal(la, lb) and torch.equal(a[..., 32:], b[..., 32:])
