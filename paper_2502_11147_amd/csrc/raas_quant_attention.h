@@ -16,7 +16,6 @@ namespace qnt {
 template <int N>
 struct Pieces {
     u32x4 p[N];
-    __device__ __forceinline__ Pieces() {}
     __device__ __forceinline__ explicit Pieces(const float (&x)[8]) {
         float y[8];
 #pragma unroll
@@ -209,17 +208,15 @@ __device__ __forceinline__ void for_split_rows(const QuantView& L, const QuantAt
 // -inf, never NaN.
 constexpr float kSlack = 8.0f, kLowest = -1e30f;
 
-// Logits (unscaled) of a block's keys and RT tiles of 16 rows. (v_mfma_scale_f32_
-// 16x16x128_f8f6f4 takes keys of 4 bits as they are stored, beside a query as two e4m3
-// numbers, and saves the 36 conversions of a block; but its sums are off by up to
-// 1.3e-5 of the products' magnitudes, a hundred times what these are: a log-sum-exp
-// was off by 3e-4.) A row of this lane's
-// column sees tokens below lim[t] of the block; `masked`: some row does not see all.
-template <typename T, int D, int KB, int VB, int RT>
-__device__ __forceinline__ void block_logits(const Block<D, KB, VB>& blk, const u32x4 (&q)[RT][D / 32][kQueryPieces<T>],
-                                             bool masked, const int (&lim)[RT], int a, f32x4 (&x)[RT][2]) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t) x[t][0] = x[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+// Logits (unscaled) of a block's keys and 16 rows. (v_mfma_scale_f32_16x16x128_f8f6f4
+// takes keys of 4 bits as they are stored, beside a query as two e4m3 numbers, and saves
+// the 36 conversions of a block; but its sums are off by up to 1.3e-5 of the products'
+// magnitudes, a hundred times what these are: a log-sum-exp was off by 3e-4.) The row of
+// this lane's column sees tokens below lim of the block; `masked`: some row does not see all.
+template <typename T, int D, int KB, int VB>
+__device__ __forceinline__ void block_logits(const Block<D, KB, VB>& blk, const u32x4 (&q)[D / 32][kQueryPieces<T>],
+                                             bool masked, int lim, int a, f32x4 (&x)[2]) {
+    x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const float scale = blk.key_scale(c);
@@ -227,44 +224,31 @@ __device__ __forceinline__ void block_logits(const Block<D, KB, VB>& blk, const 
         for (int ks = 0; ks < D / 32; ++ks) {
             const u32x4 k = blk.key(c, ks, scale);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int n = 0; n < kQueryPieces<T>; ++n) x[t][c] = mfma(k, q[t][ks][n], x[t][c]);
+            for (int n = 0; n < kQueryPieces<T>; ++n) x[c] = mfma(k, q[ks][n], x[c]);
         }
     }
     if (masked) {
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[t][c][e] = 8 * a + 4 * c + e < lim[t] ? x[t][c][e] : -INFINITY;
+            for (int e = 0; e < 4; ++e) x[c][e] = 8 * a + 4 * c + e < lim ? x[c][e] : -INFINITY;
     }
 }
 
-// Lets the rows' references follow their logits: to 2^-raise of the largest.
-template <int D, int RT>
-__device__ __forceinline__ void follow(const f32x4 (&x)[RT][2], float scale_log2, float raise, Softmax<D> (&s)[RT]) {
-    float mb[RT];
-    bool over = false;
+// Lets the rows' references follow their logits.
+template <int D>
+__device__ __forceinline__ void follow(const f32x4 (&x)[2], float scale_log2, Softmax<D>& s) {
+    float mb = x[0][0];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        mb[t] = x[t][0][0];
+    for (int j = 1; j < 8; ++j) mb = fmaxf(mb, x[j >> 2][j & 3]);
+    mb *= scale_log2;
+    if (__ballot(mb > s.m + kSlack) == 0ull) return;
+    const float m = fmaxf(s.m, max_groups(mb));
+    const float alpha = __builtin_amdgcn_exp2f(s.m - m);
+    s.l *= alpha;
 #pragma unroll
-        for (int j = 1; j < 8; ++j) mb[t] = fmaxf(mb[t], x[t][j >> 2][j & 3]);
-        mb[t] = __builtin_fmaf(mb[t], scale_log2, -raise);
-        over = over || mb[t] > s[t].m + kSlack;
-    }
-    if (__ballot(over) == 0ull) return;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const float m = fmaxf(s[t].m, max_groups(mb[t]));
-        const float alpha = __builtin_amdgcn_exp2f(s[t].m - m);
-        s[t].l *= alpha;
-#pragma unroll
-        for (int ct = 0; ct < D / 16; ++ct) s[t].o[ct] *= alpha;
-        s[t].m = m;
-    }
+    for (int ct = 0; ct < D / 16; ++ct) s.o[ct] *= alpha;
+    s.m = m;
 }
 
 // A block some of whose tokens not every row sees, with NaN among its values: a product
@@ -290,27 +274,22 @@ __device__ __forceinline__ void hand_out_nan(Block<D, KB, VB>& blk, int lim, int
         }
 }
 
-// One block against RT tiles of 16 rows.
-template <typename T, int D, int KB, int VB, int RT>
-__device__ __forceinline__ void attend_block(const Block<D, KB, VB>& blk, const u32x4 (&q)[RT][D / 32][kQueryPieces<T>],
-                                             bool masked, const int (&lim)[RT], int a, float scale_log2,
-                                             Softmax<D> (&s)[RT]) {
+// One block against 16 rows.
+template <typename T, int D, int KB, int VB>
+__device__ __forceinline__ void attend_block(const Block<D, KB, VB>& blk, const u32x4 (&q)[D / 32][kQueryPieces<T>],
+                                             bool masked, int lim, int a, float scale_log2, Softmax<D>& s) {
     constexpr int NP = kProbPieces<T>;
-    f32x4 x[RT][2];
-    block_logits<T, D, KB, VB, RT>(blk, q, masked, lim, a, x);
-    follow<D, RT>(x, scale_log2, 0.0f, s);
-    Pieces<NP> p[RT];
+    f32x4 x[2];
+    block_logits<T, D, KB, VB>(blk, q, masked, lim, a, x);
+    follow<D>(x, scale_log2, s);
+    float y[8], l = 0.0f;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        float y[8], l = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][j >> 2][j & 3], scale_log2, -s[t].m));
-            l += y[j];
-        }
-        s[t].l += l;
-        p[t] = Pieces<NP>(y);
+    for (int j = 0; j < 8; ++j) {
+        y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j >> 2][j & 3], scale_log2, -s.m));
+        l += y[j];
     }
+    s.l += l;
+    const Pieces<NP> p(y);
     float vs[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) vs[j] = blk.value_scale(j);
@@ -319,12 +298,10 @@ __device__ __forceinline__ void attend_block(const Block<D, KB, VB>& blk, const 
         u32x4 even, odd;
         blk.template values<M>(vs, even, odd);
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int n = 0; n < NP; ++n) {
-                s[t].o[2 * M] = mfma(even, p[t].p[n], s[t].o[2 * M]);
-                s[t].o[2 * M + 1] = mfma(odd, p[t].p[n], s[t].o[2 * M + 1]);
-            }
+        for (int n = 0; n < NP; ++n) {
+            s.o[2 * M] = mfma(even, p.p[n], s.o[2 * M]);
+            s.o[2 * M + 1] = mfma(odd, p.p[n], s.o[2 * M + 1]);
+        }
     };
     two(Int<0>());
     two(Int<1>());

@@ -175,12 +175,12 @@ void k_quant_stream(QuantView L, QuantAttention io) {
     const int first = w.tile * kStreamRows, rows = min(kStreamRows, w.rows - first), count = w.rows / L.G;
     // a row sees the tokens up to its own: query i of `count` lies at tokens - count + i
     auto limit = [&](int row) { return w.tokens - count + 1 + row / L.G; };
-    u32x4 q[1][F::KS][kQueryPieces<T>];
-    load_query<T, D>((const T*)io.q + row_at(L, io, w, first + col) * D, col < rows, a, q[0]);
+    u32x4 q[F::KS][kQueryPieces<T>];
+    load_query<T, D>((const T*)io.q + row_at(L, io, w, first + col) * D, col < rows, a, q);
     const int lim = col < rows ? limit(first + col) : 0;
-    Softmax<D> s[1];
-    s[0].clear();
-    s[0].m = kLowest;
+    Softmax<D> s;
+    s.clear();
+    s.m = kLowest;
     const int most = max(0, limit(first + rows - 1)), least = limit(first);
     const int nb = blocks_of(most), per = (nb + w.parts - 1) / w.parts;
     const int lo = min(nb, w.part * per), hi = min(nb, lo + per);
@@ -210,8 +210,7 @@ void k_quant_stream(QuantView L, QuantAttention io) {
     // different wavefronts take, each as its last.
     static_assert(kStreamRows <= kQuantBlock && NW >= 2, "");
     auto attend = [&](int b, Block<D, KB, VB>& blk, bool masked) {
-        const int l[1] = {lim - b * kQuantBlock};
-        attend_block<T, D, KB, VB, 1>(blk, q, masked, l, a, io.scale_log2, s);
+        attend_block<T, D, KB, VB>(blk, q, masked, lim - b * kQuantBlock, a, io.scale_log2, s);
     };
     if (turns > 0) {
         fetch(0, Int<0>());
@@ -248,13 +247,13 @@ void k_quant_stream(QuantView L, QuantAttention io) {
                                          lane);
             if (t0 + kQuantBlock > w.tokens) blk.zero_values_from(w.tokens - t0, a);
             const bool masked = t0 + kQuantBlock > least;
-            if (masked && __ballot(any_nan(blk.ve)) != 0ull) hand_out_nan<D, KB, VB>(blk, lim - t0, a, s[0]);
+            if (masked && __ballot(any_nan(blk.ve)) != 0ull) hand_out_nan<D, KB, VB>(blk, lim - t0, a, s);
             attend(b, blk, masked);
         }
     }
-    const float sum = sum_groups(s[0].l);
+    const float sum = sum_groups(s.l);
     if (a == 0) {
-        s_m[wv][col] = s[0].m;
+        s_m[wv][col] = s.m;
         s_l[wv][col] = sum;
     }
 #pragma unroll
@@ -262,7 +261,7 @@ void k_quant_stream(QuantView L, QuantAttention io) {
 #pragma unroll
         for (int ct = 0; ct < F::VC; ct += 4)
             *reinterpret_cast<f32x4*>(&s_o[wv][col][(4 * a + r) * F::VC + ct]) =
-                f32x4{s[0].o[ct][r], s[0].o[ct + 1][r], s[0].o[ct + 2][r], s[0].o[ct + 3][r]};
+                f32x4{s.o[ct][r], s.o[ct + 1][r], s.o[ct + 2][r], s.o[ct + 3][r]};
     __syncthreads();
     auto o = [&](int k, int row, int c) { return *reinterpret_cast<const f32x4*>(&s_o[k][row][c]); };
     if (w.parts == 1) {

@@ -181,16 +181,15 @@ struct Values {
             }
         }
     }
-    // times 2^by
-    __device__ __forceinline__ float value_scale(int j, int by = 0) const {
-        return __uint_as_float(scale_bits(ve[j >> 2], j & 3) + ((uint32_t)by << 23));
+    __device__ __forceinline__ float value_scale(int j) const {
+        return __uint_as_float(scale_bits(ve[j >> 2], j & 3));
     }
-    // Channels 2 M and 2 M + 1 of this lane's values of token j, as bf16 or (HALF) fp16.
-    template <int M, bool HALF = false>
+    // Channels 2 M and 2 M + 1 of this lane's values of token j, as bf16.
+    template <int M>
     __device__ __forceinline__ uint32_t value2(int j, float scale) const {
         constexpr int IN_HALF = F::VC / 4;  // pairs of channels of a half
         const int at = (M / IN_HALF) * 8 * F::VHALF + j * F::VHALF + M % IN_HALF * (VB / 4);
-        return two_values<VB, HALF>(v[at >> 4][at >> 2 & 3], at & 3, scale);
+        return two_values<VB, false>(v[at >> 4][at >> 2 & 3], at & 3, scale);
     }
     // All of this lane's values of token j.
     __device__ __forceinline__ void value_row(int j, uint32_t (&x)[F::VC / 2]) const {
@@ -205,11 +204,11 @@ struct Values {
     // Channels 2 M and 2 M + 1 of all eight tokens: two operands of the product
     // with probabilities (values come in pairs of channels of one token, operands
     // in pairs of tokens of one channel).
-    template <int M, bool HALF = false>
+    template <int M>
     __device__ __forceinline__ void values(const float (&scale)[8], u32x4& even, u32x4& odd) const {
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint32_t x = value2<M, HALF>(2 * p, scale[2 * p]), y = value2<M, HALF>(2 * p + 1, scale[2 * p + 1]);
+            const uint32_t x = value2<M>(2 * p, scale[2 * p]), y = value2<M>(2 * p + 1, scale[2 * p + 1]);
             even[p] = __builtin_amdgcn_perm(y, x, 0x05040100u);
             odd[p] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
