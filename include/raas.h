@@ -448,11 +448,11 @@ raas_status raas_prompt_weights(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
  * calls may be captured into a HIP graph: a replay works on what they hold then.
  *
  * The conventions at the top hold: device tensors (aligned to their element type),
- * nothing awaited (but by the destroy), finite inputs (scaled logits within 5e8 of
- * 0, as above, values within 2^75 where attention reads them), calls on one handle,
- * and graphs of them, ordered (attention and steps share its scratch). Nothing is
- * allocated after the creation. The same calls on the same contents give the same
- * bits. A handle's calls run on the device that was current at its creation. */
+ * nothing awaited (but by the creation and the destroy), finite inputs (scaled logits
+ * within 5e8 of 0, as above, values within 2^75 where attention reads them), calls on
+ * one handle, and graphs of them, ordered (attention and steps share its scratch).
+ * Nothing is allocated after the creation. The same calls on the same contents give the
+ * same bits. A handle's calls run on the device that was current at its creation. */
 typedef struct {
     int32_t n_layers;    /* >= 1 */
     int32_t n_q_heads;   /* multiple of n_kv_heads, group G = n_q_heads/n_kv_heads <= 16 */
@@ -470,9 +470,10 @@ typedef struct {
 
 typedef struct raas_quant_cache raas_quant_cache; /* opaque */
 
-/* Validates cfg and allocates the cache in device memory. The caller releases it
- * with raas_destroy_quant_cache. Errors: RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_STATE
- * (the stream is being captured), RAAS_E_HIP. */
+/* Validates cfg, allocates the cache in device memory, clears its pages and waits for
+ * that: the cache may be used on any stream. The caller releases it with
+ * raas_destroy_quant_cache. Errors: RAAS_E_INVALID, RAAS_E_OOM, RAAS_E_STATE (the
+ * stream is being captured), RAAS_E_HIP. */
 raas_status raas_create_quant_cache(const raas_quant_config* cfg, void* stream, raas_quant_cache** out);
 
 /* Synchronises the cache's last stream and frees it. NULL is ignored. */

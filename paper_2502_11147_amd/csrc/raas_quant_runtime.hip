@@ -157,7 +157,11 @@ raas_status raas_create_quant_cache(const raas_quant_config* cfg, void* stream, 
             {(void**)&c->ml, x.rows * 2 * 4, false},
             {&c->pool, c->layer_bytes * cfg->n_layers, true},  // (a table may name tokens that no call has written)
         };
-        const raas_status sa = allocate(reqs, &c->memory, c->bytes, (hipStream_t)stream);
+        raas_status sa = allocate(reqs, &c->memory, c->bytes, (hipStream_t)stream);
+        if (sa == RAAS_OK) {  // (the first call may run on another stream)
+            const hipError_t w = hipStreamSynchronize((hipStream_t)stream);
+            if (w != hipSuccess) sa = hip_fail(w, "hipStreamSynchronize");
+        }
         if (sa != RAAS_OK) {
             raas_destroy_quant_cache(c);
             return sa;

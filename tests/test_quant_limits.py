@@ -212,3 +212,26 @@ def test_tokens_never_written(pages, queries):
         want = np.log(n - queries + 1.0 + np.arange(queries))
         assert np.abs(_np(lse)[0] - want[:, None]).max() <= (n + 64) * U32 + 8 * U32 * want.max()
     c.close()
+
+
+@gpu
+def test_first_call_on_another_stream():
+    """A new cache is ready for every stream: clearing 9 GB does not reach into what is written at once."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    n = 140000
+    rng = np.random.default_rng(3)
+    k, v = (_dev(rng.standard_normal((1, 4, 256, 128)).astype(np.float32), torch.bfloat16) for _ in range(2))
+    table, start = _ints([[n - 1, n // 2, n - 2, 0]]), _ints([0])
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        c = raas.QuantCache(1, 4, 4, 128, n_pages=n, page_size=64, max_batch=1, key_bits=8, value_bits=8)
+        c.write(0, k, v, table, start, stream=s)
+        torch.cuda.synchronize()
+        c.read(0, ko, vo, table, start)
+        assert np.array_equal(_np(ko), ref.held(_np(k), 8)) and np.array_equal(_np(vo), ref.held(_np(v), 8))
+        c.close()
