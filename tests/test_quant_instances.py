@@ -214,3 +214,68 @@ def test_parts_joined_with_a_prefix(dtype, shape):
         sources.append(parts[0][0] + plan(hkv, len(lens) * hq // hkv, tokens, dtype == "bf16"))
         x.check(0, range(len(lens)), (p, kn[:, :tokens], vn[:, :tokens]))
     assert parts[0][0] == 64 and parts[1][0] == 1 and parts[4][0] == 12 and max(sources) > 64, (parts, sources)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("queries", [4, 12])
+def test_graphs_that_share_a_cache(queries, dtype):
+    """A captured step behind a prefix and a captured attention of a draft, of few rows and of many,
+    replayed in turn with eager work in between: lengths, inputs and the prefix as they are then."""
+    import torch
+
+    import paper_2502_11147_amd as raas
+
+    lens = [3000, 601, 5, 0, 20000]
+    x = Held(lens, 8, 2, 64, (4, 8), dtype, 64, 40, seed=queries)
+    c = raas.QuantCache(1, 8, 2, 64, n_pages=x.cache.n_pages, page_size=64, max_batch=5, max_queries=queries, key_bits=4,
+                        value_bits=8, dtype=dtype)
+    shape = (1, 2, 64 * c.n_pages, 64)
+    every = torch.arange(c.n_pages, dtype=torch.int32, device="cuda")[None]
+    c.write(0, x.data(*shape)[0], x.data(*shape)[0], every, _ints([0]))
+    p = raas.SharedPrefix(1, 8, 2, 64, 900, 5, dtype)
+    pk, pv = x.data(2, 900, 64)[0], x.data(2, 900, 64)[0]
+    p.store(0, pk, pv)
+    q, q1, k, v = (x.data(*s)[0] for s in ((5, queries, 8, 64), (5, 8, 64), (5, 2, 64), (5, 2, 64)))
+    new = lambda: (torch.zeros_like(q), torch.zeros_like(q1), torch.zeros(5, queries, 8, device="cuda"),  # noqa: E731
+                   torch.zeros(5, 8, device="cuda"))
+    n = _ints(lens)
+
+    def step(o):
+        c.decode_step(0, q1, k, v, o[1], x.table, n, lse=o[3], prefix=p)
+
+    def draft(o):
+        c.attend(0, q, o[0], x.table, n, None, o[2])
+
+    outs = new()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(outs)
+        draft(outs)
+    torch.cuda.synchronize()
+    graphs = []
+    for call in (step, draft):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(outs)
+        graphs.append(g)
+    for t in range(6):
+        n.copy_(_ints([3000 + 4 * t, 601 + t, 5 * t, -1 if t % 2 else 33, 20000 + 11 * t]))  # (in pages of their own)
+        for y in (q, q1, k, v, pk, pv):
+            y.copy_(torch.randn(y.shape, device="cuda"))
+        p.store(0, pk, pv)
+        for o in outs:
+            o.fill_(9.0)
+        torch.cuda.synchronize()
+        for g in graphs if t % 2 else graphs[::-1]:
+            g.replay()
+        got = [o.clone() for o in outs]
+        want = new()
+        for o in want:
+            o.fill_(9.0)
+        for call in (step, draft) if t % 2 else (draft, step):
+            call(want)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert not torch.isnan(b).any() and torch.equal(a, b), t
