@@ -509,7 +509,9 @@ raas_status raas_quant_read(raas_quant_cache* cache, int32_t layer, void* k, voi
  * no token has out 0 and lse -inf. A NaN group of a held value
  * reaches the channels of that group, one of a key all channels and lse, of the
  * queries that see the token, and of no other. Rows from counts[b] on, and those of
- * sequences of negative length, stay as they are. Errors: RAAS_E_INVALID, RAAS_E_HIP. */
+ * sequences of negative length, stay as they are. Beside bf16 values a probability is
+ * off by at most 2^-15 of itself in calls of up to 16 rows per KV head (queries times
+ * heads of a group), by 2^-11 beyond. Errors: RAAS_E_INVALID, RAAS_E_HIP. */
 raas_status raas_quant_attention(raas_quant_cache* cache, int32_t layer, const void* q, const int32_t* table,
                                  int32_t table_width, const int32_t* lens, const int32_t* counts, int32_t batch,
                                  int32_t queries, void* out, float* lse, void* stream);
